@@ -14,7 +14,7 @@ A case is a dict of plain values.  `kind` says which operator it is:
 
 A 4-bit row: blocks of 16 channels share a scale.  With a the block's largest magnitude the scale is the 8-bit float (5 exponent, 3
 mantissa bits: e = 0: m 2^-17, else (8 + m) 2^(e - 18)) nearest to a / 6, at least 2^-17, at most 10240, and an element is the nearest of 0, 0.5,
-1, 1.5, 2, 3, 4, 6 times the scale, with its sign; ties go to the even code.  144 bytes: 64 of K codes (channel 2 i in the low
+1, 1.5, 2, 3, 4, 6 times the scale, with its sign (a zero has none); ties go to the even code.  144 bytes: 64 of K codes (channel 2 i in the low
 half of byte i), 8 K scales, 8 V scales, 64 of V codes.
 
 Shapes are those of an 8B model (32 query heads, 8 KV heads, head dimension 128) unless a case says otherwise."""
@@ -340,7 +340,7 @@ def _encode(x):
     # (a magnitude on an edge goes to the even code: the edges below an even code belong to it)
     edge[1::2] = torch.nextafter(edge[1::2], torch.zeros_like(edge[1::2]))
     n = torch.bucketize(torch.where(fine[..., None], x.abs(), torch.zeros_like(x)) / s[..., None], edge, out_int32=True).to(torch.uint8)
-    n = torch.where(torch.signbit(x) & fine[..., None], n + 8, n).flatten(-2)
+    n = torch.where((x < 0) & (n > 0), n + 8, n).flatten(-2)
     return n[..., 0::2] | (n[..., 1::2] << 4), torch.where(fine, code, torch.full_like(code, 255)).to(torch.uint8)
 
 
