@@ -32,6 +32,15 @@
  *   kimp  [n_layers][max_batch][Hkv][max_seq_len][d']     ([1] in place of [Hkv] under TB_SCOPE_LAYER)
  *   W_K   [Hkv][D][d'] per layer (one D x d' matrix per layer AND per KV head)
  *   index lists: int32 rows of tb_index_capacity() entries, ascending token positions
+ *
+ * Rows held in 4 bits (kv_dtype = TB_FP4): kv is [n_layers][max_batch][Hkv][max_seq_len][144 bytes], a token's row pair
+ *   bytes 0..63 K codes (channel 2 i in the low, 2 i + 1 in the high half of byte i), 64..71 K scales, 72..79 V scales, 80..143 V codes.
+ * An element is code x scale, the scale shared by 16 consecutive channels.  Codes are sign and magnitude, number n = 0..7 of 0, .5, 1,
+ * 1.5, 2, 3, 4, 6 (bit 3: negative); a scale byte e m (5 and 3 bits) is m 2^-17 for e = 0, else (8 + m) 2^(e - 18).  tb_append_kv takes bf16 rows
+ * and rounds: the scale is the one nearest to the block's largest magnitude over 6 (ties to the even byte), at least 2^-17 and at most
+ * 10240 (larger elements become +-61440), then every element goes to the nearest code (ties to the even one; a zero has no
+ * sign).  An element is then off by at most 17/96 of its block's largest magnitude while that lies in [6 2^-14, 61440].  A block with an infinity or a NaN reads as
+ * NaN throughout (scale byte 255).  Every call reads the values that the codes stand for, which bf16 holds exactly.
  */
 #ifndef TOKENBUTLER_H_
 #define TOKENBUTLER_H_
@@ -55,7 +64,9 @@ typedef enum {
     TB_ERR_BAD_INDEX = -8     /* device status: caller-supplied index outside [0, L)           */
 } tb_status;
 
-typedef enum { TB_F32 = 0, TB_BF16 = 1 } tb_dtype;
+/* TB_FP4 (tb_config.kv_dtype and the allocation-free attention only): the K|V cache alone is held in 4 bits; everything
+ * else -- appended and read rows, queries, projected keys, W_K -- is bf16.  See "Rows held in 4 bits" below. */
+typedef enum { TB_F32 = 0, TB_BF16 = 1, TB_FP4 = 2 } tb_dtype;
 /* How the g importance queries of a GQA group become one ranking per KV head: a token's score is the
  * sum (default) or the largest of the group's g head scores.  TB_PER_QHEAD asks for no reduction: it is
  * accepted by a context whose lists are per query head (TB_SCOPE_Q_HEAD below), where it is the only
@@ -83,7 +94,7 @@ typedef enum { TB_NEIGHBOR_DILATE = 0, TB_NEIGHBOR_CLUSTER = 1 } tb_neighbor_mod
 
 typedef struct {
     int32_t n_layers, n_q_heads, n_kv_heads, head_dim, imp_dim;
-    int32_t kv_dtype;      /* tb_dtype                                                       */
+    int32_t kv_dtype;      /* tb_dtype of the K|V cache; TB_FP4: bf16 for all else             */
     int32_t max_batch;     /* sequences the caches hold                                      */
     int32_t max_seq_len;   /* token capacity per sequence                                    */
     int32_t max_budget;    /* largest `budget` any select call will use                      */
@@ -142,9 +153,40 @@ tb_status tb_get_length(const tb_ctx* ctx, int32_t layer, int32_t seq, int32_t* 
 /* Sec. 3.3: write new tokens' K and V rows at the end of each listed sequence, for layers
  * [layer_begin, layer_begin+layer_count).  k_dev, v_dev: [layer_count][sum(n_new)][Hkv][D], the
  * tokens of the listed sequences concatenated in list order.  seq_ids == NULL means 0..n_seq-1.
+ * Under TB_FP4 the rows are bf16, 16-byte aligned (TB_ERR_INVALID_ARG), and rounded on the way in.
  * TB_ERR_CAPACITY if any sequence would exceed max_seq_len (nothing is written). */
 tb_status tb_append_kv(tb_ctx* ctx, int32_t layer_begin, int32_t layer_count, const int32_t* seq_ids,
                        const int32_t* n_new, int32_t n_seq, const void* k_dev, const void* v_dev, void* stream);
+
+/* Rows out of the cache as values, the inverse of tb_append_kv: positions [pos_begin[i], pos_end[i]) of each listed sequence for layers
+ * [layer_begin, layer_begin+layer_count) go to k_out, v_out [layer_count][sum(pos_end - pos_begin)][Hkv][D] in the type that tb_append_kv takes
+ * (TB_FP4: bf16, exact).  What attention among the tokens of a prompt has to use when the cache does not hold them as they came.
+ * Positions must be cached (TB_ERR_INVALID_ARG); k_out, v_out 16-byte aligned device memory, not inside the cache. */
+tb_status tb_read_kv(tb_ctx* ctx, int32_t layer_begin, int32_t layer_count, const int32_t* seq_ids, const int32_t* pos_begin,
+                     const int32_t* pos_end, int32_t n_seq, void* k_out_dev, void* v_out_dev, void* stream);
+
+/* Copies a sequence into other slots, in every layer (parallel samples, beams, a shared prompt): the K|V rows and projected keys of its
+ * first n_tokens tokens, after which the slots in dst_seqs[0..n_dst) have that length and, as far as the source has, its projected length.
+ * n_tokens < 0 copies all tokens and the stored selections too (a sample can go on in the middle of an interval); otherwise the copies have
+ * no selection yet.  What the slots held is gone; the source is unchanged.  The bound resident rows and the Important buffer of the copies are
+ * brought up to date.  With device lengths the source's counters are read, and the copies' written, on the device: n_tokens < 0 can be
+ * captured and replayed while the source grows.
+ * TB_ERR_INVALID_ARG: a slot out of range, twice in dst_seqs or equal to the source, more tokens than a layer holds; TB_ERR_UNSUPPORTED: over 64 slots. */
+tb_status tb_fork_sequence(tb_ctx* ctx, int32_t src_seq, const int32_t* dst_seqs, int32_t n_dst, int32_t n_tokens, void* stream);
+
+/* Drops tokens of the listed sequences in place, in every layer (rejected drafts, rollback, a branch that keeps part of its context):
+ * tokens before keep_begin[i] stay, then come the n_keep[i] tokens at positions keep_idx_dev[i][0..n_keep[i]), which ascend strictly and lie in
+ * [keep_begin[i], length); the rest is gone and the length is keep_begin[i] + n_keep[i].  keep_idx_dev [n_seq][keep_stride] int32, device
+ * memory; n_keep == keep_idx_dev == NULL keeps nothing behind keep_begin (truncation: without device lengths or resident rows no kernel
+ * runs).  Rows and projected keys move, bit for bit; rows behind the new length are left as they are.  A layer's stored
+ * selection stays if it was made while the layer held at most keep_begin[i] tokens (without device lengths), else it is dropped.  Bound resident rows are brought up to date.
+ * An entry that does not ascend or lies outside the range sets TB_ERR_BAD_INDEX in the status word; its row holds what it held before.
+ * With device lengths the counts are still those given here: a sequence that is shorter than they say keeps its rows and length, and is reported as
+ * TB_ERR_BAD_INDEX.
+ * TB_ERR_INVALID_ARG: keep_begin + n_keep beyond a layer's length, n_keep beyond keep_stride; TB_ERR_UNPROJECTED: tokens are
+ * kept behind keep_begin of which some are projected and some not. */
+tb_status tb_compact_sequences(tb_ctx* ctx, const int32_t* seq_ids, int32_t n_seq, const int32_t* keep_begin, const int32_t* n_keep,
+                               const int32_t* keep_idx_dev, int32_t keep_stride, void* stream);
 
 /* Sec. 3.1 "Key-cache projection" K_imp = K W_K for token positions [pos_begin[i], pos_end[i]) of
  * each listed sequence (fp32 accumulation -- tensor-core tiles for bf16 storage, an FMA chain in
@@ -190,7 +232,7 @@ tb_status tb_select_topk(tb_ctx* ctx, int32_t layer_begin, int32_t layer_count, 
  * K/V row shared by the g query heads of its KV head (by no one under TB_SCOPE_Q_HEAD, where every
  * query head gathers its own list's rows; under TB_SCOPE_LAYER every KV head reads the layer's one
  * list); split over the rows with a fixed partition and
- * merged in a fixed order (bit-reproducible).  q_dev [layer_count][n_seq][Hq][D] kv_dtype;
+ * merged in a fixed order (bit-reproducible).  q_dev [layer_count][n_seq][Hq][D] kv_dtype (TB_FP4: bf16, 16-byte aligned);
  * out_dev [layer_count][n_seq][Hq][D] fp32; lse_dev (optional) [layer_count][n_seq][Hq] natural-log
  * sum-exp of the scaled logits.  idx_dev/cnt_dev: caller lists laid out like tb_select_topk's
  * outputs, or both NULL to use the lists stored by the last selection (TB_ERR_STATE if none).
@@ -210,7 +252,8 @@ tb_status tb_sparse_decode_attention(tb_ctx* ctx, int32_t layer_begin, int32_t l
  * live in a fixed array inside the library image, about 1.1 MB that every GPU loading the library
  * holds until the process exits.  The call itself allocates and frees nothing.
  *
- *   kv_dev     one layer's cache [slot][Hkv][max_seq_len][2][D] in kv_dtype (same row layout as above)
+ *   kv_dev     one layer's cache [slot][Hkv][max_seq_len][2][D] in kv_dtype (same row layout as above; TB_FP4: 144-byte rows, bf16
+ *              queries, both 16-byte aligned)
  *   seq_slots  (host, NULL = 0..n_seq-1) cache slot of each listed sequence; seq_lens (host) tokens cached
  *   q_dev      [n_seq][Hq][D] kv_dtype;  out_dev [n_seq][Hq][D] fp32;  lse_dev optional [n_seq][Hq]
  *   idx_dev / cnt_dev  caller lists [n_seq][Hkv][idx_stride] / [n_seq][Hkv] (ascending positions inside the

@@ -15,7 +15,7 @@ from .build import calls_abi, calls_match
 TB_OK = 0
 TB_ERR_INVALID_ARG, TB_ERR_UNSUPPORTED, TB_ERR_CAPACITY, TB_ERR_UNPROJECTED = -1, -2, -3, -4
 TB_ERR_STATE, TB_ERR_CUDA, TB_ERR_TIMEOUT, TB_ERR_BAD_INDEX = -5, -6, -7, -8
-TB_F32, TB_BF16 = 0, 1
+TB_F32, TB_BF16, TB_FP4 = 0, 1, 2
 TB_GROUP_SUM, TB_GROUP_MAX, TB_PER_QHEAD = 0, 1, 2
 TB_SCOPE_KV_HEAD, TB_SCOPE_Q_HEAD, TB_SCOPE_LAYER = 0, 1, 2
 TB_NEIGHBOR_DILATE, TB_NEIGHBOR_CLUSTER = 0, 1
@@ -25,7 +25,7 @@ LIB_PATH = os.path.join(_HERE, "libtokenbutler.so")
 CALLS_PATH = os.path.join(_HERE, "_tokenbutler.so")
 
 EXPORTS = ["tb_query_sizes", "tb_create", "tb_destroy", "tb_index_capacity", "tb_set_projection", "tb_reset_sequence",
-           "tb_get_length", "tb_append_kv", "tb_project_keys", "tb_score_tokens", "tb_select_topk",
+           "tb_get_length", "tb_append_kv", "tb_read_kv", "tb_fork_sequence", "tb_compact_sequences", "tb_project_keys", "tb_score_tokens", "tb_select_topk",
            "tb_sparse_decode_attention", "tb_sparse_decode_attention_static", "tb_static_get_status", "tb_predict_importance_queries", "tb_get_status", "tb_set_wait_diagnostics", "tb_use_device_lengths", "tb_sync_lengths", "tb_resident_rows_bytes", "tb_bind_resident_rows", "tb_important_buffer_bytes", "tb_bind_important_buffer", "tb_last_step_bytes", "tb_launch_count", "tb_status_string"]
 
 
@@ -82,6 +82,9 @@ def lib():
         L.tb_reset_sequence.argtypes = [vp, i32]
         L.tb_get_length.argtypes = [vp, i32, i32, ip, ip]
         L.tb_append_kv.argtypes = [vp, i32, i32, ip, ip, i32, vp, vp, vp]
+        L.tb_read_kv.argtypes = [vp, i32, i32, ip, ip, ip, i32, vp, vp, vp]
+        L.tb_fork_sequence.argtypes = [vp, i32, ip, i32, i32, vp]
+        L.tb_compact_sequences.argtypes = [vp, ip, i32, ip, ip, vp, i32, vp]
         L.tb_project_keys.argtypes = [vp, i32, i32, ip, ip, ip, i32, vp]
         L.tb_score_tokens.argtypes = [vp, i32, ip, i32, vp, i32, C.c_float, vp, vp]
         L.tb_select_topk.argtypes = [vp, i32, i32, ip, i32, vp, C.POINTER(tb_select_params), vp, vp, vp]
@@ -132,7 +135,11 @@ def select_params(budget, sinks=0, recent=0, radius=0, nmode=TB_NEIGHBOR_DILATE,
 
 
 def torch_dtype(kv_dtype):
-    return torch.bfloat16 if kv_dtype == TB_BF16 else torch.float32
+    """What a context of this type takes and returns (rows held in 4 bits enter and leave as bf16)."""
+    return torch.float32 if kv_dtype == TB_F32 else torch.bfloat16
+
+
+FP4_ROW_BYTES = 144       # a token's K|V row pair held in 4 bits
 
 
 TB_STATIC_MAX_QHEADS = 64
@@ -189,12 +196,13 @@ class Context:
         self.device = torch.device("cuda", device)
         torch.cuda.set_device(self.device)
         dt = torch_dtype(kv_dtype)
-        es = 2 if kv_dtype == TB_BF16 else 4
+        es = 4 if kv_dtype == TB_F32 else 2
+        kv_dt, kv_row = (torch.uint8, (FP4_ROW_BYTES,)) if kv_dtype == TB_FP4 else (dt, (2, head_dim))
         # caller-owned regions; kv / kimp exposed as typed views in the documented layouts
         # (kv_on_host: the cache in page-locked host memory, addressed by the device through the same pointer)
-        kv_flat = torch.empty(self.sizes[0] // es, dtype=dt, pin_memory=True) if kv_on_host else \
-            torch.empty(self.sizes[0] // es, dtype=dt, device=self.device)
-        self.kv = kv_flat.view(n_layers, max_batch, n_kv_heads, max_seq_len, 2, head_dim)
+        n_kv = self.sizes[0] // kv_dt.itemsize
+        kv_flat = torch.empty(n_kv, dtype=kv_dt, pin_memory=True) if kv_on_host else torch.empty(n_kv, dtype=kv_dt, device=self.device)
+        self.kv = kv_flat.view(n_layers, max_batch, n_kv_heads, max_seq_len, *kv_row)
         self.kimp = torch.empty(self.sizes[1] // es, dtype=dt, device=self.device).view(
             n_layers, max_batch, self.n_key_heads, max_seq_len, imp_dim)
         self.state = torch.empty(self.sizes[2], dtype=torch.uint8, device=self.device)
@@ -238,6 +246,25 @@ class Context:
         st = _calls.append_kv(self._address, layer_begin, layer_count, seq_ids, n_new, k, v, stream)
         if st:
             raise TBError(st, "tb_append_kv")
+
+    def read_kv(self, layer_begin, layer_count, seq_ids, pos_begin, pos_end, k_out, v_out, stream=None):
+        """K and V rows of positions [pos_begin[i], pos_end[i]) into k_out, v_out [layer_count, sum of them, kv heads, head dim]."""
+        st = _calls.read_kv(self._address, layer_begin, layer_count, seq_ids, pos_begin, pos_end, k_out, v_out, stream)
+        if st:
+            raise TBError(st, "tb_read_kv")
+
+    def fork_sequence(self, src_seq, dst_seqs, n_tokens=-1, stream=None):
+        """Copies the first n_tokens tokens of a sequence (-1: all, with its stored selections) into other slots."""
+        st = _calls.fork_sequence(self._address, src_seq, dst_seqs, n_tokens, stream)
+        if st:
+            raise TBError(st, "tb_fork_sequence")
+
+    def compact_sequences(self, seq_ids, keep_begin, n_keep=None, keep_idx=None, stream=None):
+        """Keeps the first keep_begin[i] tokens and the n_keep[i] at positions keep_idx[i] ([sequences, stride] int32, on the device);
+        without n_keep and keep_idx: those first tokens alone."""
+        st = _calls.compact_sequences(self._address, seq_ids, keep_begin, n_keep, keep_idx, stream)
+        if st:
+            raise TBError(st, "tb_compact_sequences")
 
     def project_keys(self, layer_begin, layer_count, seq_ids, pos_begin, pos_end, stream=None, n_seq=None):
         """pos_begin = pos_end = None: every listed sequence's unprojected tokens (n_seq says how many sequences)."""

@@ -12,7 +12,8 @@ namespace {
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-int elem_size(int dtype) { return dtype == TB_BF16 ? 2 : 4; }
+int elem_size(int dtype) { return dtype == TB_F32 ? 4 : 2; }        // of everything but a 4-bit cache's rows
+int row_bytes(const tb_config* c) { return c->kv_dtype == TB_FP4 ? 144 : 2 * c->head_dim * elem_size(c->kv_dtype); }
 
 struct Layout {
     size_t kv_bytes, kimp_bytes;
@@ -35,7 +36,7 @@ tb_status check_config(const tb_config* c) {
         c->max_budget <= 0 || c->max_radius < 0 || c->device < 0)
         return TB_ERR_INVALID_ARG;
     if (c->n_q_heads % c->n_kv_heads != 0) return TB_ERR_INVALID_ARG;
-    if (c->kv_dtype != TB_F32 && c->kv_dtype != TB_BF16) return TB_ERR_INVALID_ARG;
+    if (c->kv_dtype != TB_F32 && c->kv_dtype != TB_BF16 && c->kv_dtype != TB_FP4) return TB_ERR_INVALID_ARG;
     if (c->list_scope != TB_SCOPE_KV_HEAD && c->list_scope != TB_SCOPE_Q_HEAD && c->list_scope != TB_SCOPE_LAYER) return TB_ERR_INVALID_ARG;
     if (c->head_dim != 128) return TB_ERR_UNSUPPORTED;
     if (c->imp_dim != 16 && c->imp_dim != 32) return TB_ERR_UNSUPPORTED;
@@ -53,7 +54,7 @@ void compute_layout(const tb_config* c, Layout* l) {
     scope_heads(c, &hi, &hl, &ha);
     const size_t pairs = (size_t)c->n_layers * c->max_batch;
     const size_t units = pairs * hl;                                   // index lists
-    l->kv_bytes = pairs * c->n_kv_heads * c->max_seq_len * 2 * c->head_dim * es;
+    l->kv_bytes = pairs * c->n_kv_heads * c->max_seq_len * row_bytes(c);
     l->kimp_bytes = pairs * hi * c->max_seq_len * c->imp_dim * es;
     l->idx_cap = (int)align_up((size_t)(2 * c->max_radius + 1) * c->max_budget, 4);
     l->sel_stride = (int)align_up((size_t)c->max_budget, 4);
@@ -93,7 +94,7 @@ tb_status make_kimp_map(tb_ctx* c) {
         return TB_ERR_CUDA;
     const tb_config& g = c->cfg;
     const int es = elem_size(g.kv_dtype);
-    const int row_bytes = g.imp_dim * es;
+    const int row_bytes = g.imp_dim * es;              // of a projected key
     cuuint64_t dims[2] = {(cuuint64_t)g.imp_dim, (cuuint64_t)g.n_layers * g.max_batch * c->geom.Hi * g.max_seq_len};
     cuuint64_t strides[1] = {(cuuint64_t)row_bytes};
     cuuint32_t box[2] = {(cuuint32_t)g.imp_dim, 256u};
@@ -101,7 +102,7 @@ tb_status make_kimp_map(tb_ctx* c) {
     CUtensorMapSwizzle sw = row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B
                             : row_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
                                               : CU_TENSOR_MAP_SWIZZLE_32B;
-    CUresult r = ((EncodeTiledFn)fn)(&c->kimp_map, g.kv_dtype == TB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
+    CUresult r = ((EncodeTiledFn)fn)(&c->kimp_map, c->geom.dtype == TB_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32,
                                      2, c->kimp, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, sw,
                                      CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? TB_OK : TB_ERR_CUDA;
@@ -225,9 +226,9 @@ tb_status tb_create(const tb_config* cfg, void* kv, void* kimp, void* state, voi
     scope_heads(cfg, &g.Hi, &g.Hl, &g.Ha);
     g.gl = cfg->list_scope == TB_SCOPE_KV_HEAD ? g.g : 1, g.ga = g.Hq / g.Ha;
     g.D = cfg->head_dim, g.dp = cfg->imp_dim, g.max_batch = cfg->max_batch, g.max_seq_len = cfg->max_seq_len;
-    g.idx_cap = l.idx_cap, g.dtype = cfg->kv_dtype;
+    g.idx_cap = l.idx_cap, g.fp4 = cfg->kv_dtype == TB_FP4, g.dtype = g.fp4 ? (int)TB_BF16 : cfg->kv_dtype, g.row_bytes = row_bytes(cfg);
     const size_t n = (size_t)cfg->n_layers * cfg->max_batch;
-    c->len.assign(n, 0), c->len_proj.assign(n, 0), c->has_sel.assign(n, 0), c->sel_cnt.assign(n, -1);
+    c->len.assign(n, 0), c->len_proj.assign(n, 0), c->has_sel.assign(n, 0), c->sel_cnt.assign(n, -1), c->sel_len.assign(n, 0);
     c->last_bytes = 0, c->launches = 0;
     c->wait_poll_limit = 0, c->drop_tile = -1;
     c->dev_lengths = 0, c->growth_reserve = 0;
@@ -293,6 +294,7 @@ tb_status tb_get_length(const tb_ctx* c, int32_t layer, int32_t seq, int32_t* le
 tb_status tb_append_kv(tb_ctx* c, int32_t lb, int32_t lc, const int32_t* seq_ids, const int32_t* n_new, int32_t n_seq,
                        const void* k, const void* v, void* stream) {
     if (!c || !n_new || !k || !v || bad_layers(c, lb, lc)) return TB_ERR_INVALID_ARG;
+    if (c->geom.fp4 && (((uintptr_t)k | (uintptr_t)v) & 15)) return TB_ERR_INVALID_ARG;
     int seqs[kMaxLaunchSeq];
     tb_status st = resolve_seqs(c, seq_ids, n_seq, seqs);
     if (st != TB_OK) return st;
@@ -496,6 +498,7 @@ tb_status tb_select_topk(tb_ctx* c, int32_t lb, int32_t lc, const int32_t* seq_i
                 cand_range(c->len[u], p->sinks, p->recent, &lo, &hi);
                 // without neighbour expansion the stored count is known here: min(budget, candidates)
                 c->sel_cnt[u] = p->radius == 0 ? (p->budget < hi - lo ? p->budget : hi - lo) : -1;
+                c->sel_len[u] = c->dev_lengths ? c->cfg.max_seq_len : c->len[u];
             }
         c->last_bytes = bytes;
     }
@@ -507,6 +510,7 @@ tb_status tb_sparse_decode_attention(tb_ctx* c, int32_t lb, int32_t lc, const in
                                      float* out, float* lse, void* stream) {
     if (!c || !q || !p || !out || bad_layers(c, lb, lc)) return TB_ERR_INVALID_ARG;
     if ((idx == nullptr) != (cnt == nullptr)) return TB_ERR_INVALID_ARG;
+    if (c->geom.fp4 && ((uintptr_t)q & 15)) return TB_ERR_INVALID_ARG;
     const bool dense = p->budget < 0;
     if (!dense && (p->sinks < 0 || p->recent < 0 || p->radius < 0)) return TB_ERR_INVALID_ARG;
     int seqs[kMaxLaunchSeq];
@@ -531,7 +535,7 @@ tb_status tb_sparse_decode_attention(tb_ctx* c, int32_t lb, int32_t lc, const in
                 rows = (long long)(p->sinks < L ? p->sinks : L) + bound + p->recent;
                 if (rows > L) rows = L;
             }
-            bytes += (uint64_t)rows * c->geom.Ha * 2 * c->cfg.head_dim * elem_size(c->cfg.kv_dtype);
+            bytes += (uint64_t)rows * c->geom.Ha * c->geom.row_bytes;
         }
     const int step = layers_per_launch(n_seq);
     const size_t es = elem_size(c->cfg.kv_dtype);
@@ -564,6 +568,142 @@ tb_status tb_sparse_decode_attention(tb_ctx* c, int32_t lb, int32_t lc, const in
     return TB_OK;
 }
 
+tb_status tb_read_kv(tb_ctx* c, int32_t lb, int32_t lc, const int32_t* seq_ids, const int32_t* pos_begin, const int32_t* pos_end,
+                     int32_t n_seq, void* k_out, void* v_out, void* stream) {
+    if (!c || !pos_begin || !pos_end || !k_out || !v_out || bad_layers(c, lb, lc)) return TB_ERR_INVALID_ARG;
+    if (((uintptr_t)k_out | (uintptr_t)v_out) & 15) return TB_ERR_INVALID_ARG;
+    int seqs[kMaxLaunchSeq];
+    const tb_status st = resolve_seqs(c, seq_ids, n_seq, seqs);
+    if (st != TB_OK) return st;
+    ReadTable rt;
+    rt.tok_off[0] = 0;
+    int longest = 0;
+    long long total = 0;
+    for (int i = 0; i < n_seq; ++i) {
+        if (pos_begin[i] < 0 || pos_end[i] < pos_begin[i]) return TB_ERR_INVALID_ARG;
+        for (int l = lb; l < lb + lc; ++l)
+            if (pos_end[i] > c->len[(size_t)l * c->cfg.max_batch + seqs[i]]) return TB_ERR_INVALID_ARG;      // beyond the cached tokens
+        const int n = pos_end[i] - pos_begin[i];
+        if (n > longest) longest = n;
+        if ((total += n) > 2147483647LL) return TB_ERR_CAPACITY;
+        rt.pos_begin[i] = pos_begin[i], rt.tok_off[i + 1] = (int)total;
+    }
+    if (longest == 0) return TB_OK;
+    const size_t layer_stride = (size_t)total * c->cfg.n_kv_heads * c->cfg.head_dim * elem_size(c->cfg.kv_dtype);
+    const int step = layers_per_launch(n_seq);
+    for (int l0 = lb; l0 < lb + lc; l0 += step) {
+        const int n = l0 + step <= lb + lc ? step : lb + lc - l0;
+        UnitTable ut;
+        fill_table(c, &ut, l0, n, seqs, n_seq);
+        if (launch_read(c, ut, rt, longest, (char*)k_out + (size_t)(l0 - lb) * layer_stride, (char*)v_out + (size_t)(l0 - lb) * layer_stride,
+                        (cudaStream_t)stream) != cudaSuccess)
+            return TB_ERR_CUDA;
+        c->launches++;
+    }
+    return TB_OK;
+}
+
+namespace {
+// What the optional copies hold of the listed sequences, whose rows or lists a kernel has just written.
+tb_status refresh_copies(tb_ctx* c, const int* seqs, int n_seq, bool lists, cudaStream_t stream) {
+    const int step = layers_per_launch(n_seq);
+    for (int l0 = 0; l0 < c->cfg.n_layers; l0 += step) {
+        UnitTable ut;
+        fill_table(c, &ut, l0, l0 + step <= c->cfg.n_layers ? step : c->cfg.n_layers - l0, seqs, n_seq);
+        if (c->res_rows) {
+            if (launch_refresh_resident(c, ut, stream) != cudaSuccess) return TB_ERR_CUDA;
+            c->last_cache_write = (long long)c->launches, c->launches++;
+        }
+        if (lists && c->imp_rows) {
+            if (launch_migrate(c, ut, stream) != cudaSuccess) return TB_ERR_CUDA;
+            c->last_list_write = (long long)c->launches, c->launches++;
+        }
+    }
+    return TB_OK;
+}
+}  // namespace
+
+tb_status tb_fork_sequence(tb_ctx* c, int32_t src, const int32_t* dst, int32_t n_dst, int32_t n_tokens, void* stream) {
+    if (!c || !dst || src < 0 || src >= c->cfg.max_batch) return TB_ERR_INVALID_ARG;
+    ForkArgs a;
+    const tb_status st = resolve_seqs(c, dst, n_dst, a.dst);
+    if (st != TB_OK) return st;
+    for (int i = 0; i < n_dst; ++i)
+        if (a.dst[i] == src) return TB_ERR_INVALID_ARG;
+    const int mb = c->cfg.max_batch, layers = c->cfg.n_layers;
+    bool selected = false, cached = c->dev_lengths != 0;
+    for (int l = 0; l < layers; ++l) {
+        const size_t u = (size_t)l * mb + src;
+        if (n_tokens > c->len[u]) return TB_ERR_INVALID_ARG;
+        selected |= n_tokens < 0 && c->has_sel[u], cached |= c->len[u] > 0 && n_tokens != 0;
+    }
+    a.src = src, a.n_dst = n_dst, a.n_tokens = n_tokens < 0 ? -1 : n_tokens;
+    const int step = layers_per_launch(1);
+    for (int l0 = 0; cached && l0 < layers; l0 += step) {
+        UnitTable ut;
+        fill_table(c, &ut, l0, l0 + step <= layers ? step : layers - l0, &src, 1);
+        a.max_tokens = 0;
+        for (int l = 0; l < ut.layer_count; ++l) {
+            const int n = n_tokens >= 0 && n_tokens < ut.len[l] ? n_tokens : ut.len[l];
+            if (n > a.max_tokens) a.max_tokens = n;
+        }
+        if (launch_fork(c, ut, a, (cudaStream_t)stream) != cudaSuccess) return TB_ERR_CUDA;
+        c->last_cache_write = c->last_list_write = (long long)c->launches;
+        c->launches++;
+    }
+    for (int l = 0; l < layers; ++l)
+        for (int i = 0; i < n_dst; ++i) {
+            const size_t u = (size_t)l * mb + src, d = (size_t)l * mb + a.dst[i];
+            c->len[d] = n_tokens < 0 ? c->len[u] : n_tokens;
+            c->len_proj[d] = c->len_proj[u] < c->len[d] ? c->len_proj[u] : c->len[d];
+            c->has_sel[d] = n_tokens < 0 ? c->has_sel[u] : 0;
+            c->sel_cnt[d] = n_tokens < 0 ? c->sel_cnt[u] : -1, c->sel_len[d] = c->sel_len[u];
+        }
+    return cached ? refresh_copies(c, a.dst, n_dst, selected, (cudaStream_t)stream) : TB_OK;
+}
+
+tb_status tb_compact_sequences(tb_ctx* c, const int32_t* seq_ids, int32_t n_seq, const int32_t* keep_begin, const int32_t* n_keep,
+                               const int32_t* keep_idx, int32_t keep_stride, void* stream) {
+    if (!c || !keep_begin || (n_keep == nullptr) != (keep_idx == nullptr)) return TB_ERR_INVALID_ARG;
+    int seqs[kMaxLaunchSeq];
+    const tb_status st = resolve_seqs(c, seq_ids, n_seq, seqs);
+    if (st != TB_OK) return st;
+    const int mb = c->cfg.max_batch, layers = c->cfg.n_layers;
+    CompactArgs a;
+    a.keep = keep_idx, a.stride = keep_stride, a.max_keep = 0;
+    for (int i = 0; i < n_seq; ++i) {
+        const int n = n_keep ? n_keep[i] : 0;
+        if (keep_begin[i] < 0 || n < 0 || (n > 0 && n > keep_stride)) return TB_ERR_INVALID_ARG;
+        a.begin[i] = keep_begin[i], a.n_keep[i] = n;
+        if (n > a.max_keep) a.max_keep = n;
+        for (int l = 0; l < layers; ++l) {
+            const size_t u = (size_t)l * mb + seqs[i];
+            if ((long long)keep_begin[i] + n > c->len[u]) return TB_ERR_INVALID_ARG;
+            // kept tokens are projected or not: a prefix of them, whose length only the device knows, cannot be
+            if (n > 0 && c->len_proj[u] > keep_begin[i] && c->len_proj[u] < c->len[u]) return TB_ERR_UNPROJECTED;
+        }
+    }
+    const int step = layers_per_launch(n_seq);
+    for (int l0 = 0; (a.max_keep > 0 || c->dev_lengths) && l0 < layers; l0 += step) {
+        UnitTable ut;
+        fill_table(c, &ut, l0, l0 + step <= layers ? step : layers - l0, seqs, n_seq);
+        if (launch_compact(c, ut, a, (cudaStream_t)stream) != cudaSuccess) return TB_ERR_CUDA;
+        c->last_cache_write = (long long)c->launches;
+        c->launches++;
+    }
+    for (int l = 0; l < layers; ++l)
+        for (int i = 0; i < n_seq; ++i) {
+            const size_t u = (size_t)l * mb + seqs[i];
+            const int len = a.begin[i] + a.n_keep[i];
+            const bool all = c->len_proj[u] >= c->len[u];
+            c->len_proj[u] = all ? len : c->len_proj[u] < len ? c->len_proj[u] : len;
+            c->len[u] = len;
+            // the list may name tokens that moved or went, or that a window of the shorter sequence reaches again
+            if (c->sel_len[u] > a.begin[i]) c->has_sel[u] = 0, c->sel_cnt[u] = -1;
+        }
+    return c->res_rows ? refresh_copies(c, seqs, n_seq, false, (cudaStream_t)stream) : TB_OK;
+}
+
 tb_status tb_get_status(tb_ctx* c, void* stream, int32_t* device_status) {
     if (!c || !device_status) return TB_ERR_INVALID_ARG;
     int32_t v = 0;
@@ -576,14 +716,14 @@ tb_status tb_get_status(tb_ctx* c, void* stream, int32_t* device_status) {
 
 size_t tb_resident_rows_bytes(const tb_config* cfg, int32_t sinks, int32_t window) {
     if (check_config(cfg) != TB_OK || sinks < 0 || window < 0) return 0;
-    return (size_t)cfg->n_layers * cfg->max_batch * cfg->n_kv_heads * ((size_t)sinks + window) * 2 * cfg->head_dim * elem_size(cfg->kv_dtype);
+    return (size_t)cfg->n_layers * cfg->max_batch * cfg->n_kv_heads * ((size_t)sinks + window) * row_bytes(cfg);
 }
 
 size_t tb_important_buffer_bytes(const tb_config* cfg) {
     if (check_config(cfg) != TB_OK || cfg->list_scope != TB_SCOPE_KV_HEAD) return 0;
     Layout l;
     compute_layout(cfg, &l);
-    return (size_t)cfg->n_layers * cfg->max_batch * cfg->n_kv_heads * (size_t)l.idx_cap * 2 * cfg->head_dim * elem_size(cfg->kv_dtype);
+    return (size_t)cfg->n_layers * cfg->max_batch * cfg->n_kv_heads * (size_t)l.idx_cap * row_bytes(cfg);
 }
 
 namespace {

@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "tb_common.cuh"
+#include "tb_fp4.cuh"
 #include "tb_internal.h"
 
 namespace cg = cooperative_groups;
@@ -366,6 +367,169 @@ __device__ __forceinline__ void f32_rows(const float* __restrict__ qbase, int g,
     reinterpret_cast<float4*>(my_stage)[8 * 32 + lane] = stat;
 }
 
+// The 4-bit warp's rows (row format: tb_fp4.cuh).  Like the bf16 tiles, S = K Q^T and O^T += V^T P^T run on mma.sync m16n8k16 with 16
+// gathered tokens and the group's heads as the N = 8 columns, but on f16: codes turn into f16 pairs in one instruction, and
+// code x scale is exact there.  Both contractions take their operands in an order that leaves every lane with contiguous bytes of a row:
+//   S:  a lane (gid, tig) holds channels 32 tig .. 32 tig + 31 of two rows (16 bytes and two scales each); k-step ks takes channels
+//       32 tig + 4 ks + (0, 1 | 2, 3), and so does the query operand.
+//   O:  a lane holds the 16 channels of block gid (8 bytes and one scale) of four rows; the codes of two rows are interleaved,
+//       so that a converted pair is one channel of two tokens; tile mt is channels 16 gid + 2 mt (row gid) and + 1 (row gid + 8).
+//   Row r of a tile is token r for even r < 8, 8 + (r + 3) % 8 for odd r < 8, one more than row r - 8's for the others: 144-byte rows,
+//   unpadded, then hit distinct banks in both reads.
+// Queries are bf16: scaled by a power of two per head that brings the largest channel to [2^13, 2^14), every channel down to 2^-28 of
+// it is exact in f16 and the rest is off by less than 2^-39 of it.  Probabilities are kept 2^15 times larger (the running maximum is
+// lowered by 15, which cancels everywhere) and split into an f16 high and low part: 22 bits for all but those below 2^-29 of the
+// largest, which are off by less than 2^-40 of it.
+// Leaves accumulators and statistics parked as the bf16 warp does, but for the channels: float4 number mt * 32 + lane holds
+// channels 16 gid + 2 mt and + 1.
+constexpr int kFp4Stage = kTileTok * kFp4Row;         // 2304: two of them hold the parked values
+__device__ __forceinline__ void mma_f16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+template <int kStages, typename Tokens, typename Issue, typename Commit>
+__device__ __forceinline__ void fp4_rows(const __nv_bfloat16* __restrict__ qbase, int g, float qscale, unsigned char* my_stage, int wb, int we,
+                                         int n_tiles, uint32_t bad_bits, bool& any_bad, Tokens tokens_of, Issue issue_token, Commit commit) {
+    constexpr int D = 128;
+    const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
+    uint32_t qb[8][2];
+    float xs[2];                                       // what a score of heads 2 tig, 2 tig + 1 is multiplied by
+    {
+        uint32_t w[16];
+        uint32_t top2 = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 v = gid < g ? __ldg(reinterpret_cast<const uint4*>(qbase + gid * D + tig * 32) + i) : make_uint4(0u, 0u, 0u, 0u);
+            w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top2 = __vmaxu2(top2, w[i] & 0x7fff7fffu);
+        top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 1));
+        top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 2));
+        const uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+        const uint32_t e = min(max(top >> 7, 14u), 254u);
+        const float up = __uint_as_float((267u - e) << 23), down = __uint_as_float((e - 13u) << 23);       // 2^(140 - e), 2^(e - 140)
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) {
+            qb[ks][0] = pack_f16(bf16_lo(w[2 * ks]) * up, bf16_hi(w[2 * ks]) * up);
+            qb[ks][1] = pack_f16(bf16_lo(w[2 * ks + 1]) * up, bf16_hi(w[2 * ks + 1]) * up);
+        }
+        xs[0] = qscale * __shfl_sync(0xffffffffu, down, tig * 8), xs[1] = qscale * __shfl_sync(0xffffffffu, down, tig * 8 + 4);
+    }
+    float o[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+    const int t0 = (gid & 1) ? 8 + ((gid + 3) & 7) : gid;              // token of row gid; row gid + 8: the next
+    const uint32_t k_off = t0 * kFp4Row + tig * 16, ks_off = t0 * kFp4Row + kFp4KScales + tig * 2;
+    const int tA = 2 * tig, tB = 8 + ((2 * tig + 4) & 7);              // tokens of k = 2 tig, 2 tig + 1; k + 8: the next ones
+    const uint32_t vA_off = tA * kFp4Row, vB_off = tB * kFp4Row;
+    for (int tile = 0; tile < n_tiles; ++tile) {
+        const int r0 = wb + tile * kTileTok;
+        const bool in_range = lane < kTileTok && r0 + lane < we;
+        const bool bad = in_range && (bad_bits & 1u);
+        any_bad |= bad;
+        bad_bits >>= 1;
+        const unsigned vmask = __ballot_sync(0xffffffffu, in_range && !bad);
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+        __syncwarp();                                  // every lane's copies of this tile are visible to the warp
+        const unsigned char* st = my_stage + tile % kStages * kFp4Stage;
+        float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
+        {
+            const uint4 ka = *reinterpret_cast<const uint4*>(st + k_off), kb = *reinterpret_cast<const uint4*>(st + k_off + kFp4Row);
+            const uint32_t sa = *reinterpret_cast<const unsigned short*>(st + ks_off), sb = *reinterpret_cast<const unsigned short*>(st + ks_off + kFp4Row);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t wa = j == 0 ? ka.x : j == 1 ? ka.y : j == 2 ? ka.z : ka.w, wbw = j == 0 ? kb.x : j == 1 ? kb.y : j == 2 ? kb.z : kb.w;
+                const uint32_t fa = j < 2 ? fp4_scale_pair<0>(sa) : fp4_scale_pair<1>(sa), fb = j < 2 ? fp4_scale_pair<0>(sb) : fp4_scale_pair<1>(sb);
+                uint32_t a[4], b[4];
+                fp4_unpack(wa, a[0], a[1], a[2], a[3]);
+                fp4_unpack(wbw, b[0], b[1], b[2], b[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[i] = mul_f16x2(a[i], fa), b[i] = mul_f16x2(b[i], fb);
+                mma_f16(c0, a[0], b[0], a[1], b[1], qb[2 * j][0], qb[2 * j][1]);
+                mma_f16(c1, a[2], b[2], a[3], b[3], qb[2 * j + 1][0], qb[2 * j + 1][1]);
+            }
+        }
+        const bool v0 = (vmask >> t0) & 1u, v1 = (vmask >> (t0 + 1)) & 1u;
+        float x[4];
+        x[0] = v0 ? (c0[0] + c1[0]) * xs[0] : -INFINITY, x[1] = v0 ? (c0[1] + c1[1]) * xs[1] : -INFINITY;
+        x[2] = v1 ? (c0[2] + c1[2]) * xs[0] : -INFINITY, x[3] = v1 ? (c0[3] + c1[3]) * xs[1] : -INFINITY;
+        float tmax[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) {
+            tmax[0] = fmaxf(tmax[0], __shfl_xor_sync(0xffffffffu, tmax[0], off));
+            tmax[1] = fmaxf(tmax[1], __shfl_xor_sync(0xffffffffu, tmax[1], off));
+        }
+        float corr[2], ms[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float m_new = fmaxf(m_run[e], tmax[e] - 15.f);
+            ms[e] = m_new == -INFINITY ? 0.f : m_new;
+            corr[e] = exp2f(m_run[e] - ms[e]);
+            m_run[e] = m_new;
+        }
+        float p[4];
+        p[0] = exp2f(x[0] - ms[0]), p[1] = exp2f(x[1] - ms[1]), p[2] = exp2f(x[2] - ms[0]), p[3] = exp2f(x[3] - ms[1]);
+        l_run[0] = l_run[0] * corr[0] + p[0] + p[2];
+        l_run[1] = l_run[1] * corr[1] + p[1] + p[3];
+        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i][0] *= corr[0], o[i][1] *= corr[1], o[i][2] *= corr[0], o[i][3] *= corr[1];
+        }
+        const uint32_t h0 = pack_f16(p[0], p[1]), h1 = pack_f16(p[2], p[3]);
+        const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
+        const uint32_t bh0 = movmatrix_trans(h0), bh1 = movmatrix_trans(h1);
+        const uint32_t bl0 = movmatrix_trans(pack_f16(p[0] - f0.x, p[1] - f0.y)), bl1 = movmatrix_trans(pack_f16(p[2] - f1.x, p[3] - f1.y));
+        {
+            const unsigned char *rA = st + vA_off, *rB = st + vB_off;
+            const uint2 wA = *reinterpret_cast<const uint2*>(rA + kFp4VCodes + gid * 8), wB = *reinterpret_cast<const uint2*>(rB + kFp4VCodes + gid * 8);
+            const uint2 wC = *reinterpret_cast<const uint2*>(rA + kFp4Row + kFp4VCodes + gid * 8), wD = *reinterpret_cast<const uint2*>(rB + kFp4Row + kFp4VCodes + gid * 8);
+            const uint32_t s01 = (rA[kFp4VScales + gid] | (uint32_t)rB[kFp4VScales + gid] << 16) << 7;
+            const uint32_t s23 = (rA[kFp4Row + kFp4VScales + gid] | (uint32_t)rB[kFp4Row + kFp4VScales + gid] << 16) << 7;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {              // eight channels of the block
+                const uint32_t a = h ? wA.y : wA.x, b = h ? wB.y : wB.x, c = h ? wC.y : wC.x, d = h ? wD.y : wD.x;
+                uint32_t e01[4], o01[4], e23[4], o23[4];               // even and odd channels of token pairs
+                fp4_unpack((a & 0x0f0f0f0fu) | ((b << 4) & 0xf0f0f0f0u), e01[0], e01[1], e01[2], e01[3]);
+                fp4_unpack(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), o01[0], o01[1], o01[2], o01[3]);
+                fp4_unpack((c & 0x0f0f0f0fu) | ((d << 4) & 0xf0f0f0f0u), e23[0], e23[1], e23[2], e23[3]);
+                fp4_unpack(((c >> 4) & 0x0f0f0f0fu) | (d & 0xf0f0f0f0u), o23[0], o23[1], o23[2], o23[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t a0 = mul_f16x2(e01[i], s01), a1 = mul_f16x2(o01[i], s01), a2 = mul_f16x2(e23[i], s23), a3 = mul_f16x2(o23[i], s23);
+                    mma_f16(o[h * 4 + i], a0, a1, a2, a3, bh0, bh1);
+                    mma_f16(o[h * 4 + i], a0, a1, a2, a3, bl0, bl1);
+                }
+            }
+        }
+        __syncwarp();                                  // the warp is done reading this stage
+        if (tile + kStages < n_tiles) {
+            const int t = tokens_of(tile + kStages);
+            bad_bits |= (uint32_t)(t < 0) << (kStages - 1);
+            issue_token(tile + kStages, max(t, 0));
+        }
+        commit();
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+    for (int off = 4; off < 32; off <<= 1) {
+        l_run[0] += __shfl_xor_sync(0xffffffffu, l_run[0], off);
+        l_run[1] += __shfl_xor_sync(0xffffffffu, l_run[1], off);
+    }
+    __syncwarp();
+    float4* park = reinterpret_cast<float4*>(my_stage);
+#pragma unroll
+    for (int mt = 0; mt < 8; ++mt) park[mt * 32 + lane] = make_float4(o[mt][0], o[mt][1], o[mt][2], o[mt][3]);
+    park[8 * 32 + lane] = make_float4(m_run[0], l_run[0], m_run[1], l_run[1]);
+}
+
 // Shared memory behind the warps' stages for the merge inside a cluster of C blocks: the accumulator slices this
 // block owns from every block ([slices per owner][C][32 lanes] float4) and every block's (m, l) ([C][4] float4).
 constexpr size_t kFourWarpBytes = 76 * 1024;       // least shared memory of a 4-warp block (see launch_attention)
@@ -378,7 +542,7 @@ static inline size_t cluster_merge_bytes(int C) { return (size_t)((8 + C - 1) / 
 // go through the global workspace and the last block to arrive merges them.
 // kSources: the resident sink / window copies or the Important buffer are bound and a row reference names
 // its source; without them (the usual case) the gather carries no trace of the option.
-// FG: 0 = bf16 storage; else fp32 storage with up to FG query heads per unit.
+// FG: 0 = bf16 storage, -1 = rows held in 4 bits; else fp32 storage with up to FG query heads per unit.
 template <int NW, int kMmaStages, bool kSources = false, int FG = 0>
 __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut, AttnArgs a, const void* __restrict__ kv,
                                                            const int32_t* __restrict__ state_idx,
@@ -386,9 +550,13 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
                                                            float* __restrict__ part_ml, uint32_t* __restrict__ counters,
                                                            int32_t* __restrict__ status) {
     constexpr int D = 128;
-    constexpr bool kF32 = FG > 0;
+    constexpr bool kF32 = FG > 0, kFp4 = FG < 0;
     constexpr int kTok = kF32 ? 8 : kTileTok;          // rows of a stage
-    constexpr int kRowBytes = 2 * D * (kF32 ? 4 : 2);  // a K|V row pair
+    constexpr int kRowBytes = kFp4 ? kFp4Row : 2 * D * (kF32 ? 4 : 2);  // a K|V row pair
+    constexpr int kStage = kFp4 ? kFp4Stage : kStageBytes;
+    // the channels of parked accumulator tile mt of lane ln: this one, and the one kPairStep further
+    constexpr int kPairStep = kFp4 ? 1 : 8;
+    auto channel = [](int mt, int ln) { return kFp4 ? (ln >> 2) * 16 + 2 * mt : mt * 16 + (ln >> 2); };
     extern __shared__ __align__(128) unsigned char smem_dyn[];
     __shared__ int sh_last;
 
@@ -449,7 +617,7 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
     const int we = min(r_end, wb + (tiles_lo + (warp < tiles_rem ? 1 : 0)) * kTok);
     const int n_tiles = (we - wb + kTok - 1) / kTok;
 
-    unsigned char* my_stage = smem_dyn + (size_t)warp * kMmaStages * kStageBytes;
+    unsigned char* my_stage = smem_dyn + (size_t)warp * kMmaStages * kStage;
     // the unit's rows in the cache and in the optional copies (see RowMap)
     const unsigned char* kv_unit = reinterpret_cast<const unsigned char*>(kv) + au.kv_c * gm.max_seq_len * kRowBytes;
     const unsigned char* res_unit = reinterpret_cast<const unsigned char*>(a.res_rows) + au.kv_c * (size_t)(a.res_sinks + a.res_window) * kRowBytes;
@@ -468,7 +636,26 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
     // kMmaStages-1 groups are complete" always means "the tile about to be used has landed".
     const uint32_t stage_u32 = smem_u32(my_stage);
     auto issue_token = [&](int tile, int t) {     // t: lane i < kTok holds the token of row i
-        const uint32_t dst = stage_u32 + (tile % kMmaStages) * kStageBytes;
+        const uint32_t dst = stage_u32 + (tile % kMmaStages) * kStage;
+        if constexpr (kFp4) {
+            // nine 16-byte chunks per row, chunk after chunk: four and a half instructions of the warp per tile
+            constexpr int kChunks = kRowBytes / 16;
+#pragma unroll
+            for (int i = 0; i < (kTok * kChunks + 31) / 32; ++i) {
+                const int item = i * 32 + lane, r = item / kChunks;
+                const int ti = __shfl_sync(0xffffffffu, t, min(r, kTok - 1));
+                const unsigned char* src = kv_unit;
+                int row = ti;
+                if constexpr (kSources) {
+                    const int which = ti >> kRowSrcShift;
+                    src = which == 0 ? kv_unit : which == 1 ? res_unit : imp_unit;
+                    row = ti & kRowIdxMask;
+                }
+                if (item < kTok * kChunks)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + item * 16), "l"(src + (size_t)row * kRowBytes + (item - r * kChunks) * 16) : "memory");
+            }
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < kTok; ++i) {
             const int ti = __shfl_sync(0xffffffffu, t, i);
@@ -529,6 +716,8 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
     float4* tbuf = reinterpret_cast<float4*>(my_stage);
     if constexpr (kF32) {
         f32_rows<FG, kMmaStages>(reinterpret_cast<const float*>(a.q) + hq0 * D, g, qscale, my_stage, wb, we, n_tiles, bad_bits, any_bad, tokens_of, issue_token, commit);
+    } else if constexpr (kFp4) {
+        fp4_rows<kMmaStages>(reinterpret_cast<const __nv_bfloat16*>(a.q) + hq0 * D, g, qscale, my_stage, wb, we, n_tiles, bad_bits, any_bad, tokens_of, issue_token, commit);
     } else {
         // Q^T as the B operand of S = K Q^T: k = channels, n = query heads (gid; heads >= g are zero padding)
         uint32_t qb[8][2];
@@ -724,8 +913,8 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
 
     // ---- the warps' results become the block's, the blocks' the problem's -------------------------------
     __syncthreads();
-    auto warp_buf = [&](int w) { return reinterpret_cast<const float4*>(smem_dyn + (size_t)w * kMmaStages * kStageBytes); };
-    // block result of slot (mt, ln): acc = (head 2tg ch, head 2tg+1 ch, head 2tg ch+8, head 2tg+1 ch+8), ch = mt*16 + ln/4
+    auto warp_buf = [&](int w) { return reinterpret_cast<const float4*>(smem_dyn + (size_t)w * kMmaStages * kStage); };
+    // block result of slot (mt, ln): acc = (head 2tg ch, head 2tg+1 ch, head 2tg ch', head 2tg+1 ch'), ch = channel(mt, ln), ch' = ch + kPairStep
     auto fold_slot = [&](int mt, int ln, float4& acc, float4& stat) {
         float4 q[NW];
 #pragma unroll
@@ -756,17 +945,17 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
         cg::cluster_group cluster = cg::this_cluster();
         const int rank = (int)cluster.block_rank(), C = (int)cluster.num_blocks();
         const int T = (8 + C - 1) / C;                               // slices per owner
-        float4* area = reinterpret_cast<float4*>(smem_dyn + (size_t)NW * kMmaStages * kStageBytes);   // [T][C][32 lanes]
+        float4* area = reinterpret_cast<float4*>(smem_dyn + (size_t)NW * kMmaStages * kStage);   // [T][C][32 lanes]
         float4* ml = area + (size_t)T * C * 32;                      // [C][4]: (m, l) of heads 2 tig, 2 tig + 1
-        // writes one merged piece: (acc, sums ls0 / ls1, maxima M0 / M1) of heads 2 tg, 2 tg + 1 at channels ch, ch + 8
+        // writes one merged piece: (acc, sums ls0 / ls1, maxima M0 / M1) of heads 2 tg, 2 tg + 1 at channels ch, ch + kPairStep
         auto write_piece = [&](int tg, int ch, const float4& acc, float M0, float ls0, float M1, float ls1) {
             const int u0 = 2 * tg, u1 = u0 + 1;
             if (u0 < g) {
-                a.out[(hq0 + u0) * D + ch] = acc.x / ls0, a.out[(hq0 + u0) * D + ch + 8] = acc.z / ls0;
+                a.out[(hq0 + u0) * D + ch] = acc.x / ls0, a.out[(hq0 + u0) * D + ch + kPairStep] = acc.z / ls0;
                 if (a.lse && ch == 0) a.lse[hq0 + u0] = (M0 + log2f(ls0)) * kLn2;
             }
             if (u1 < g) {
-                a.out[(hq0 + u1) * D + ch] = acc.y / ls1, a.out[(hq0 + u1) * D + ch + 8] = acc.w / ls1;
+                a.out[(hq0 + u1) * D + ch] = acc.y / ls1, a.out[(hq0 + u1) * D + ch + kPairStep] = acc.w / ls1;
                 if (a.lse && ch == 0) a.lse[hq0 + u1] = (M1 + log2f(ls1)) * kLn2;
             }
         };
@@ -775,7 +964,7 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
                 const int mt = slot >> 5, ln = slot & 31;
                 float4 acc, stat;
                 fold_slot(mt, ln, acc, stat);
-                write_piece(ln & 3, mt * 16 + (ln >> 2), acc, stat.x, stat.y, stat.z, stat.w);
+                write_piece(ln & 3, channel(mt, ln), acc, stat.x, stat.y, stat.z, stat.w);
             }
             attn_stamp(6);
             return;
@@ -815,7 +1004,7 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
                     acc.x = fmaf(v[r].x, e0, acc.x), acc.y = fmaf(v[r].y, e1, acc.y);
                     acc.z = fmaf(v[r].z, e0, acc.z), acc.w = fmaf(v[r].w, e1, acc.w);
                 }
-                write_piece(tg, j * 16 + (ln >> 2), acc, M0, ls0, M1, ls1);
+                write_piece(tg, channel(j, ln), acc, M0, ls0, M1, ls1);
             }
         };
         if (rank < 8) {
@@ -827,15 +1016,15 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
         // splits through the global workspace, merged by the last block to arrive
         SplitSink sink{part_o, part_ml, counters, a.out, a.lse, hq0, lu, split, a.nsplit};
         for (int slot = tid; slot < 256; slot += NW * 32) {
-            const int mt = slot >> 5, ln = slot & 31, u0 = 2 * (ln & 3), ch = mt * 16 + (ln >> 2);
+            const int mt = slot >> 5, ln = slot & 31, u0 = 2 * (ln & 3), ch = channel(mt, ln);
             float4 acc, stat;
             fold_slot(mt, ln, acc, stat);
             if (u0 < g) {
-                sink.publish_at(u0, ch, acc.x), sink.publish_at(u0, ch + 8, acc.z);
+                sink.publish_at(u0, ch, acc.x), sink.publish_at(u0, ch + kPairStep, acc.z);
                 if (mt == 0 && ln < 4) sink.publish_stat(u0, stat.x, stat.y);
             }
             if (u0 + 1 < g) {
-                sink.publish_at(u0 + 1, ch, acc.y), sink.publish_at(u0 + 1, ch + 8, acc.w);
+                sink.publish_at(u0 + 1, ch, acc.y), sink.publish_at(u0 + 1, ch + kPairStep, acc.w);
                 if (mt == 0 && ln < 4) sink.publish_stat(u0 + 1, stat.z, stat.w);
             }
         }
@@ -843,6 +1032,9 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
     }
     attn_stamp(6);
 }
+
+// Stages per warp of the 4-bit kernels: 18 KB of rows in flight (14 KB where 12 warps share an SM).
+constexpr int fp4_stages(int nw) { return nw == 12 ? 6 : 8; }
 
 static int pick_nsplit(const tb_ctx* c, int units, int max_rows) {
     // about two blocks per SM and never a thin second wave: with 64 problems of 9.8K rows (which now take two 12-warp
@@ -892,6 +1084,11 @@ cudaError_t launch_attention(const tb_ctx* c, const UnitTable& ut, const AttnArg
                 prepare(attn_mma_kernel<4, 2, true, G>, 113, true), prepare(attn_mma_kernel<8, 2, true, G>, 220, true);
                 prepare(attn_mma_kernel<8, 3, true, G>, 220, true);
             };
+            auto prepare_fp4 = [&](auto warps) {
+                constexpr int W = decltype(warps)::value;
+                prepare(attn_mma_kernel<W, fp4_stages(W), false, -1>, W == 4 ? 113 : 220, true), prepare(attn_mma_kernel<W, fp4_stages(W), true, -1>, W == 4 ? 113 : 220, true);
+            };
+            prepare_fp4(std::integral_constant<int, 4>{}), prepare_fp4(std::integral_constant<int, 8>{}), prepare_fp4(std::integral_constant<int, 12>{});
             prepare_f32(std::integral_constant<int, 1>{}), prepare_f32(std::integral_constant<int, 2>{});
             prepare_f32(std::integral_constant<int, 4>{}), prepare_f32(std::integral_constant<int, 8>{});
             (void)cudaGetLastError();
@@ -1009,7 +1206,7 @@ cudaError_t launch_attention(const tb_ctx* c, const UnitTable& ut, const AttnArg
         const size_t merge_bytes = a.cluster_merge ? cluster_merge_bytes(a.nsplit) : 0;
         // three stages per warp when the 8-warp block still fits the SM with them
         const int nst = (nw == 8 && 8 * 3 * kStageBytes + merge_bytes <= 220 * 1024 && a.nsplit <= 8) ? 3 : 2;
-        size_t smem = (size_t)nw * nst * kStageBytes + merge_bytes;
+        size_t smem = (gm.fp4 ? (size_t)nw * fp4_stages(nw) * kFp4Stage : (size_t)nw * nst * kStageBytes) + merge_bytes;
         // The split count of the 4-warp launches is chosen for two blocks per SM; their 64 KB of stages would let
         // a third one in, and the block scheduler then loads some SMs with three blocks and leaves others with one
         // (batch 8 at 64K: 59 us per launch against 52.6).  Asking for a third of the SM's shared memory plus a
@@ -1044,6 +1241,13 @@ cudaError_t launch_attention(const tb_ctx* c, const UnitTable& ut, const AttnArg
             return launch_f32(std::integral_constant<int, 8>{});
         }
         const bool sources = a.res_rows != nullptr || a.imp_rows != nullptr;
+        if (gm.fp4) {
+            auto launch_fp4 = [&](auto warps) {
+                constexpr int W = decltype(warps)::value;
+                return sources ? launch(attn_mma_kernel<W, fp4_stages(W), true, -1>) : launch(attn_mma_kernel<W, fp4_stages(W), false, -1>);
+            };
+            return nw == 12 ? launch_fp4(std::integral_constant<int, 12>{}) : nw == 8 ? launch_fp4(std::integral_constant<int, 8>{}) : launch_fp4(std::integral_constant<int, 4>{});
+        }
 #define TB_MMA(NW_, ST_) (sources ? launch(attn_mma_kernel<NW_, ST_, true>) : launch(attn_mma_kernel<NW_, ST_, false>))
         if (nw == 12) return TB_MMA(12, 2);
         if (nw == 8 && nst == 3) return TB_MMA(8, 3);
@@ -1091,7 +1295,7 @@ tb_status static_scratch_for_current_device(unsigned char** out, int* sm_count) 
         int sms = 0;
         if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return TB_ERR_CUDA;
         const auto prepare = [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 113 * 1024) == cudaSuccess; };
-        if (!prepare(tb::attn_mma_kernel<4, 2>) || !prepare(tb::attn_mma_kernel<4, 2, true, 1>) || !prepare(tb::attn_mma_kernel<4, 2, true, 2>) ||
+        if (!prepare(tb::attn_mma_kernel<4, 2>) || !prepare(tb::attn_mma_kernel<4, tb::fp4_stages(4), false, -1>) || !prepare(tb::attn_mma_kernel<4, 2, true, 1>) || !prepare(tb::attn_mma_kernel<4, 2, true, 2>) ||
             !prepare(tb::attn_mma_kernel<4, 2, true, 4>) || !prepare(tb::attn_mma_kernel<4, 2, true, 8>))
             return TB_ERR_CUDA;
         g_sm_count[dev] = sms;
@@ -1115,7 +1319,8 @@ extern "C" tb_status tb_sparse_decode_attention_static(const void* kv_dev, int32
         return TB_ERR_INVALID_ARG;
     if ((idx_dev == nullptr) != (cnt_dev == nullptr) || sinks < 0 || recent < 0) return TB_ERR_INVALID_ARG;
     if (idx_dev && idx_stride <= 0) return TB_ERR_INVALID_ARG;
-    if (kv_dtype != TB_F32 && kv_dtype != TB_BF16) return TB_ERR_INVALID_ARG;
+    if (kv_dtype != TB_F32 && kv_dtype != TB_BF16 && kv_dtype != TB_FP4) return TB_ERR_INVALID_ARG;
+    if (kv_dtype == TB_FP4 && (((uintptr_t)q_dev | (uintptr_t)kv_dev) & 15)) return TB_ERR_INVALID_ARG;
     if (n_q_heads % n_kv_heads != 0) return TB_ERR_INVALID_ARG;
     if (head_dim != 128 || n_q_heads / n_kv_heads > kMaxGroup) return TB_ERR_UNSUPPORTED;
     // the fixed scratch bounds the problem: refuse anything larger instead of overrunning it
@@ -1145,7 +1350,8 @@ extern "C" tb_status tb_sparse_decode_attention_static(const void* kv_dev, int32
     Geom gm;
     gm.n_layers = 1, gm.Hq = n_q_heads, gm.Hkv = n_kv_heads, gm.g = n_q_heads / n_kv_heads, gm.D = head_dim, gm.dp = 0;
     gm.Hi = gm.Hl = gm.Ha = n_kv_heads, gm.gl = gm.ga = gm.g;
-    gm.max_batch = 1 << 20, gm.max_seq_len = max_seq_len, gm.idx_cap = idx_dev ? idx_stride : 0, gm.dtype = kv_dtype;
+    gm.max_batch = 1 << 20, gm.max_seq_len = max_seq_len, gm.idx_cap = idx_dev ? idx_stride : 0;
+    gm.fp4 = kv_dtype == TB_FP4, gm.dtype = gm.fp4 ? (int)TB_BF16 : kv_dtype, gm.row_bytes = gm.fp4 ? kFp4Row : kv_dtype == TB_BF16 ? 512 : 1024;
     UnitTable ut;
     ut.layer_begin = 0, ut.layer_count = 1, ut.n_seq = n_seq;
     ut.use_dev_len = 0, ut.len_is_projected = 0, ut.len_dev = nullptr, ut.len_proj_dev = nullptr;   // lengths are the caller's
@@ -1187,9 +1393,11 @@ extern "C" tb_status tb_sparse_decode_attention_static(const void* kv_dev, int32
     dim3 grid(a.nsplit, n_kv_heads, n_seq);
     // the stored-list arguments of the kernels are never read here (caller lists or dense)
     const auto launch = [&](auto kernel) {
-        kernel<<<grid, kAttnThreads, kAttnWarps * 2 * kStageBytes, s>>>(gm, ut, a, kv_dev, nullptr, nullptr, part_o, part_ml, counters, status);
+        const size_t smem = gm.fp4 ? kAttnWarps * fp4_stages(kAttnWarps) * kFp4Stage : kAttnWarps * 2 * kStageBytes;
+        kernel<<<grid, kAttnThreads, smem, s>>>(gm, ut, a, kv_dev, nullptr, nullptr, part_o, part_ml, counters, status);
     };
-    if (kv_dtype == TB_BF16) launch(attn_mma_kernel<4, 2>);
+    if (gm.fp4) launch(attn_mma_kernel<kAttnWarps, fp4_stages(kAttnWarps), false, -1>);
+    else if (kv_dtype == TB_BF16) launch(attn_mma_kernel<4, 2>);
     else if (gm.ga == 1) launch(attn_mma_kernel<4, 2, true, 1>);
     else if (gm.ga == 2) launch(attn_mma_kernel<4, 2, true, 2>);
     else if (gm.ga <= 4) launch(attn_mma_kernel<4, 2, true, 4>);

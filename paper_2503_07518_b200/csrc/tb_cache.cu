@@ -6,11 +6,6 @@
 
 namespace tb {
 
-struct AppendTable {
-    int tok_off[kMaxLaunchSeq + 1];  // prefix sums of n_new over the listed sequences
-    int blk_off[kMaxLaunchSeq + 1];  // and of the blocks that copy them
-};
-
 // A block belongs to one (layer, sequence); a warp moves 512 contiguous bytes of the cache at a time (a bf16 K|V row
 // pair, or half an fp32 one), kAppendUnroll of them in flight: a copy of 16 bytes per thread and no division per
 // element.  Bound by DRAM bandwidth for prompts and by the launch for a decode token.  32K tokens x 8 heads, one layer
@@ -69,21 +64,12 @@ __global__ void __launch_bounds__(kAppendThreads) append_kernel(Geom gm, UnitTab
             }
         }
     }
-    // (only when the kernels read the device counters: otherwise the host's mirrors carry the lengths and
-    // the counters are brought up to date when that mode is switched on)
-    if (ut.use_dev_len && last_block_arrives(counter, gridDim.x * gridDim.y)) {
-        for (int i = threadIdx.x; i < ut.layer_count * ut.n_seq; i += blockDim.x) {
-            const int l2 = i / ut.n_seq, s2 = i % ut.n_seq;
-            const size_t pair = (size_t)(ut.layer_begin + l2) * gm.max_batch + ut.seq_id[s2];
-            const int base = unit_len(gm, ut, l2, s2), n = at.tok_off[s2 + 1] - at.tok_off[s2];
-            if (base + n > gm.max_seq_len) atomicExch(status, kStatusCapacity);
-            else len_dev[pair] = base + n;
-        }
-    }
+    append_finish(gm, ut, at, len_dev, counter, status);
 }
 
 cudaError_t launch_append(const tb_ctx* c, const UnitTable& ut, const int* n_new, const int* tok_off, int total_new,
                           const void* k, const void* v, cudaStream_t s) {
+    if (c->geom.fp4) return launch_append_fp4(c, ut, n_new, tok_off, total_new, k, v, s);
     AppendTable at;
     for (int i = 0; i <= ut.n_seq; ++i) at.tok_off[i] = tok_off[i];
     const Geom& gm = c->geom;
@@ -109,21 +95,47 @@ cudaError_t launch_append(const tb_ctx* c, const UnitTable& ut, const int* n_new
 }
 
 // ---------------------------------------------------------------------------------------------
+// Rows back out of the cache, as tb_append_kv takes them: [layer][token][head][D], 16 bytes per thread.
+template <typename T>
+__global__ void __launch_bounds__(256) read_kernel(Geom gm, UnitTable ut, ReadTable rt, const T* __restrict__ kv, T* __restrict__ k_out, T* __restrict__ v_out) {
+    constexpr int D = 128, kChunks = D / Elem<T>::kPer16, kPairs = 256 / (2 * kChunks);      // chunks of a row, row pairs of a block's pass
+    const int ll = blockIdx.z, s = blockIdx.y;
+    const unsigned n_pair = (unsigned)(rt.tok_off[s + 1] - rt.tok_off[s]) * gm.Hkv, hkv = gm.Hkv;
+    const unsigned j = threadIdx.x % (2 * kChunks);
+    const size_t unit0 = ((size_t)(ut.layer_begin + ll) * gm.max_batch + ut.seq_id[s]) * gm.Hkv;
+    const size_t dst0 = ((size_t)ll * rt.tok_off[ut.n_seq] + rt.tok_off[s]) * gm.Hkv;
+    for (unsigned pair = blockIdx.x * kPairs + threadIdx.x / (2 * kChunks); pair < n_pair; pair += gridDim.x * kPairs) {
+        const unsigned tok = pair / hkv, h = pair - tok * hkv;
+        const uint4 v = reinterpret_cast<const uint4*>(kv + ((unit0 + h) * gm.max_seq_len + rt.pos_begin[s] + tok) * 2 * D)[j];
+        reinterpret_cast<uint4*>((j < kChunks ? k_out : v_out) + (dst0 + pair) * D)[j % kChunks] = v;
+    }
+}
+
+cudaError_t launch_read(const tb_ctx* c, const UnitTable& ut, const ReadTable& rt, int max_tokens, void* k, void* v, cudaStream_t s) {
+    const Geom& gm = c->geom;
+    if (gm.fp4) return launch_read_fp4(c, ut, rt, max_tokens, k, v, s);
+    const int pairs = gm.dtype == TB_BF16 ? 8 : 4;     // per pass of a block
+    const long long blocks = ((long long)max_tokens * gm.Hkv + pairs - 1) / pairs;
+    dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536), ut.n_seq, ut.layer_count);
+    if (gm.dtype == TB_BF16) read_kernel<<<grid, 256, 0, s>>>(gm, ut, rt, (const __nv_bfloat16*)c->kv, (__nv_bfloat16*)k, (__nv_bfloat16*)v);
+    else read_kernel<<<grid, 256, 0, s>>>(gm, ut, rt, (const float*)c->kv, (float*)k, (float*)v);
+    return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
 // KV migration (paper Sec. 3.3: on a prediction step the selected K/V pairs are moved into the contiguous
 // Important buffer, from which the following steps attend): rows list[j] of the cache -> row j of the
 // unit's buffer, 16 bytes per thread.  One block column per list; the count is read on the device.
-template <typename T>
-__global__ void __launch_bounds__(256) migrate_kernel(Geom gm, UnitTable ut, const T* __restrict__ kv, const int32_t* __restrict__ state_idx,
-                                                      const int32_t* __restrict__ state_cnt, T* __restrict__ imp) {
-    constexpr int kPer16 = Elem<T>::kPer16;
-    const int chunks = 2 * gm.D / kPer16;              // 16-byte chunks of a K|V row pair
+__global__ void __launch_bounds__(256) migrate_kernel(Geom gm, UnitTable ut, const uint4* __restrict__ kv, const int32_t* __restrict__ state_idx,
+                                                      const int32_t* __restrict__ state_cnt, uint4* __restrict__ imp) {
+    const int chunks = gm.row_bytes / 16;              // 16-byte chunks of a K|V row pair
     const int u = blockIdx.y, h = u % gm.Hl, s = (u / gm.Hl) % ut.n_seq, ll = u / (gm.Hl * ut.n_seq);
     const size_t pc = (size_t)(ut.layer_begin + ll) * gm.max_batch + ut.seq_id[s];
     const size_t lc = pc * gm.Hl + h, kc = pc * gm.Hkv + h;               // lists are per KV head here
     const int n = min(state_cnt[lc], gm.idx_cap);
     const int32_t* list = state_idx + lc * gm.idx_cap;
-    const uint4* src = reinterpret_cast<const uint4*>(kv + kc * gm.max_seq_len * 2 * gm.D);
-    uint4* dst = reinterpret_cast<uint4*>(imp + lc * (size_t)gm.idx_cap * 2 * gm.D);
+    const uint4* src = kv + kc * gm.max_seq_len * chunks;
+    uint4* dst = imp + lc * (size_t)gm.idx_cap * chunks;
     for (long long w = (long long)blockIdx.x * blockDim.x + threadIdx.x; w < (long long)n * chunks; w += (long long)gridDim.x * blockDim.x) {
         const int j = (int)(w / chunks), c = (int)(w % chunks);
         dst[(size_t)j * chunks + c] = src[(size_t)list[j] * chunks + c];
@@ -136,42 +148,12 @@ cudaError_t launch_migrate(const tb_ctx* c, const UnitTable& ut, cudaStream_t s)
     int bx = 2 * c->sm_count / units;                  // about two blocks per SM over the launch
     bx = bx < 1 ? 1 : bx > 64 ? 64 : bx;
     dim3 grid(bx, units);
-    if (gm.dtype == TB_BF16)
-        migrate_kernel<__nv_bfloat16><<<grid, 256, 0, s>>>(gm, ut, (const __nv_bfloat16*)c->kv, c->st.idx, c->st.cnt, (__nv_bfloat16*)c->imp_rows);
-    else
-        migrate_kernel<float><<<grid, 256, 0, s>>>(gm, ut, (const float*)c->kv, c->st.idx, c->st.cnt, (float*)c->imp_rows);
+    migrate_kernel<<<grid, 256, 0, s>>>(gm, ut, (const uint4*)c->kv, c->st.idx, c->st.cnt, (uint4*)c->imp_rows);
     return cudaGetLastError();
 }
 
 // ---------------------------------------------------------------------------------------------
 // K_imp[t][j] = round( sum_c K[t][c] * W[c][j] ), channels in ascending order, fp32 FMA chain.
-
-struct ProjectTable {
-    int auto_range;                  // 1: [projected length, length) of every (layer, sequence), from the device counters
-    int pos_begin[kMaxLaunchSeq];
-    int pos_end[kMaxLaunchSeq];
-};
-
-// Token range of a projection block's (layer, sequence).
-__device__ __forceinline__ void project_range(const Geom& gm, const UnitTable& ut, const ProjectTable& pt, int ll, int s, int& begin, int& end) {
-    if (pt.auto_range) {
-        const size_t pair = (size_t)(ut.layer_begin + ll) * gm.max_batch + ut.seq_id[s];
-        begin = ut.len_proj_dev[pair], end = ut.len_dev[pair];
-    } else {
-        begin = pt.pos_begin[s], end = pt.pos_end[s];
-    }
-}
-// The last block of a projection launch to finish advances the device counters of the projected lengths.
-__device__ __forceinline__ void project_finish(const Geom& gm, const UnitTable& ut, const ProjectTable& pt, int32_t* len_proj_dev,
-                                               uint32_t* counter) {
-    if (!ut.use_dev_len || !last_block_arrives(counter, gridDim.x * gridDim.y * gridDim.z)) return;
-    for (int i = threadIdx.x; i < ut.layer_count * ut.n_seq; i += blockDim.x) {
-        int b, e;
-        project_range(gm, ut, pt, i / ut.n_seq, i % ut.n_seq, b, e);
-        const size_t pair = (size_t)(ut.layer_begin + i / ut.n_seq) * gm.max_batch + ut.seq_id[i % ut.n_seq];
-        if (e > len_proj_dev[pair]) len_proj_dev[pair] = e;
-    }
-}
 
 // fp32 storage: CUDA-core tiles of 64 tokens x d' outputs, 8 outputs of DP / 16 tokens per thread, so that the FMA
 // units and not the shared-memory reads bound it (per four channels and token: a 16-byte read of K and, shared by the
@@ -376,6 +358,7 @@ cudaError_t launch_project(const tb_ctx* c, const UnitTable& ut, const int* pos_
     }
     if (max_range <= 0) return cudaSuccess;
     const Geom& gm = c->geom;
+    if (gm.fp4) return launch_project_fp4(c, ut, pt, max_range, s);
     if (gm.dtype == TB_BF16) {
         dim3 grid_mma((max_range + kPmTokens - 1) / kPmTokens, gm.Hi, ut.layer_count * ut.n_seq);
         const __nv_bfloat16* kvp = (const __nv_bfloat16*)c->kv;

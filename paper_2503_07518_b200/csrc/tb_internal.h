@@ -28,7 +28,9 @@ struct Geom {
     int Hi, Hl, Ha, gl, ga;
     int max_batch, max_seq_len;
     int idx_cap;       // entries per index-list row
-    int dtype;         // tb_dtype
+    int dtype;         // TB_F32 or TB_BF16: queries, projected keys, W_K, and the rows where they are not held in 4 bits
+    int fp4;           // 1: K|V rows are held in 4 bits (TB_FP4)
+    int row_bytes;     // of a token's K|V row pair of one KV head
 };
 
 // Per-launch table of (layer-local, sequence) pairs: which cache slot and how many tokens.
@@ -60,6 +62,35 @@ struct SelectArgs {
     int radius, nmode;
     int32_t* idx_copy;    // [layer_count][n_seq][Hl][idx_cap] or NULL
     int32_t* cnt_copy;
+};
+
+struct AppendTable {
+    int tok_off[kMaxLaunchSeq + 1];  // prefix sums of n_new over the listed sequences
+    int blk_off[kMaxLaunchSeq + 1];  // and of the blocks that copy them
+};
+
+struct ProjectTable {
+    int auto_range;                  // 1: [projected length, length) of every (layer, sequence), from the device counters
+    int pos_begin[kMaxLaunchSeq];
+    int pos_end[kMaxLaunchSeq];
+};
+
+struct ForkArgs {
+    int src, n_dst;              // slots
+    int n_tokens;                // -1: all, with the stored lists
+    int max_tokens;              // most that any layer copies
+    int dst[kMaxLaunchSeq];
+};
+struct CompactArgs {
+    const int32_t* keep;         // [n_seq][stride]
+    int stride;
+    int begin[kMaxLaunchSeq];    // tokens before these stay where they are
+    int n_keep[kMaxLaunchSeq];
+    int max_keep;
+};
+struct ReadTable {
+    int tok_off[kMaxLaunchSeq + 1];  // prefix sums of the tokens read
+    int pos_begin[kMaxLaunchSeq];
 };
 
 struct NeighborArgs {
@@ -137,6 +168,7 @@ struct tb_ctx {
     std::vector<int> len, len_proj;       // [n_layers * max_batch]
     std::vector<int> has_sel;             // [n_layers * max_batch]
     std::vector<int> sel_cnt;             // [n_layers * max_batch] stored list length when the host knows it, else -1
+    std::vector<int> sel_len;             // [n_layers * max_batch] tokens cached when the stored list was made (at most: under device lengths)
     CUtensorMap kimp_map;                 // 2-D view of kimp: rows = all token slots, cols = d'
     int tile_rows;                        // rows per TMA box of the score pass
     int sm_count;
@@ -176,6 +208,39 @@ __device__ __forceinline__ bool last_block_arrives(uint32_t* counter, unsigned n
     }
     __syncthreads();
     return s_last != 0;
+}
+
+// The last block of an append launch advances the device counters of the lengths (only when the kernels read them: otherwise the host's
+// mirrors carry the lengths and the counters are brought up to date when that mode is switched on).
+__device__ __forceinline__ void append_finish(const Geom& gm, const UnitTable& ut, const AppendTable& at, int32_t* len_dev, uint32_t* counter, int32_t* status) {
+    if (!ut.use_dev_len || !last_block_arrives(counter, gridDim.x * gridDim.y)) return;
+    for (int i = threadIdx.x; i < ut.layer_count * ut.n_seq; i += blockDim.x) {
+        const int l2 = i / ut.n_seq, s2 = i % ut.n_seq;
+        const size_t pair = (size_t)(ut.layer_begin + l2) * gm.max_batch + ut.seq_id[s2];
+        const int base = unit_len(gm, ut, l2, s2), n = at.tok_off[s2 + 1] - at.tok_off[s2];
+        if (base + n > gm.max_seq_len) atomicExch(status, kStatusCapacity);
+        else len_dev[pair] = base + n;
+    }
+}
+// Token range of a projection block's (layer, sequence).
+__device__ __forceinline__ void project_range(const Geom& gm, const UnitTable& ut, const ProjectTable& pt, int ll, int s, int& begin, int& end) {
+    if (pt.auto_range) {
+        const size_t pair = (size_t)(ut.layer_begin + ll) * gm.max_batch + ut.seq_id[s];
+        begin = ut.len_proj_dev[pair], end = ut.len_dev[pair];
+    } else {
+        begin = pt.pos_begin[s], end = pt.pos_end[s];
+    }
+}
+// The last block of a projection launch to finish advances the device counters of the projected lengths.
+__device__ __forceinline__ void project_finish(const Geom& gm, const UnitTable& ut, const ProjectTable& pt, int32_t* len_proj_dev,
+                                               uint32_t* counter) {
+    if (!ut.use_dev_len || !last_block_arrives(counter, gridDim.x * gridDim.y * gridDim.z)) return;
+    for (int i = threadIdx.x; i < ut.layer_count * ut.n_seq; i += blockDim.x) {
+        int b, e;
+        project_range(gm, ut, pt, i / ut.n_seq, i % ut.n_seq, b, e);
+        const size_t pair = (size_t)(ut.layer_begin + i / ut.n_seq) * gm.max_batch + ut.seq_id[i % ut.n_seq];
+        if (e > len_proj_dev[pair]) len_proj_dev[pair] = e;
+    }
 }
 #endif
 
@@ -232,6 +297,20 @@ cudaError_t launch_append(const tb_ctx* c, const UnitTable& ut, const int* n_new
 // pos_begin == nullptr: every listed sequence's unprojected tokens [projected length, length), taken from the
 // device counters; max_range then bounds the tokens of any one (layer, sequence)
 cudaError_t launch_project(const tb_ctx* c, const UnitTable& ut, const int* pos_begin, const int* pos_end, int max_range, cudaStream_t s);
+
+cudaError_t launch_read(const tb_ctx* c, const UnitTable& ut, const ReadTable& rt, int max_tokens, void* k, void* v, cudaStream_t s);
+
+// tb_cache_fp4.cu: the same where rows are held in 4 bits
+cudaError_t launch_append_fp4(const tb_ctx* c, const UnitTable& ut, const int* n_new, const int* tok_off, int total_new,
+                              const void* k, const void* v, cudaStream_t s);
+cudaError_t launch_project_fp4(const tb_ctx* c, const UnitTable& ut, const ProjectTable& pt, int max_range, cudaStream_t s);
+cudaError_t launch_read_fp4(const tb_ctx* c, const UnitTable& ut, const ReadTable& rt, int max_tokens, void* k, void* v, cudaStream_t s);
+
+// tb_sequence.cu
+cudaError_t launch_fork(const tb_ctx* c, const UnitTable& ut, const ForkArgs& a, cudaStream_t s);
+cudaError_t launch_compact(const tb_ctx* c, const UnitTable& ut, const CompactArgs& a, cudaStream_t s);
+// brings the resident sink and window rows of the listed sequences up to the cache's
+cudaError_t launch_refresh_resident(const tb_ctx* c, const UnitTable& ut, cudaStream_t s);
 
 // tb_select.cu
 cudaError_t launch_score(const tb_ctx* c, const UnitTable& ut, const float* q_imp, int reduce, float scale, float* scores,

@@ -123,6 +123,13 @@ bool want(Py_ssize_t got, Py_ssize_t n) {
     return false;
 }
 
+// Lists that say something about the same sequences (None: nothing).
+bool same_length(const IntList& some, const IntList& all) {
+    if (!some.data || some.n == all.n) return true;
+    PyErr_SetString(PyExc_ValueError, "lists of different lengths");
+    return false;
+}
+
 template <typename F>
 PyObject* call(F&& f) {
     tb_status st;
@@ -130,6 +137,27 @@ PyObject* call(F&& f) {
     st = f();
     Py_END_ALLOW_THREADS
     return PyLong_FromLong((long)st);
+}
+
+// A tensor (or whatever else has a shape and says where it is) and its leading sizes; `cols` may be null.
+bool read_matrix(PyObject* o, void** out, int32_t* rows, int32_t* cols) {
+    int32_t* sizes[2] = {rows, cols};
+    if (THPVariable_Check(o) && THPVariable_Unpack(o).dim() >= (cols ? 2 : 1)) {
+        const at::Tensor& t = THPVariable_Unpack(o);
+        *out = t.data_ptr();
+        for (int i = 0; i < (cols ? 2 : 1); ++i) *sizes[i] = (int32_t)t.size(i);
+        return true;
+    }
+    PyObject* shape = PyObject_GetAttr(o, g_shape);
+    if (!shape) return false;
+    bool ok = true;
+    for (int i = 0; i < (cols ? 2 : 1) && ok; ++i) {
+        PyObject* n = PySequence_GetItem(shape, i);    // (an IndexError where there are fewer)
+        ok = n && read_int(n, sizes[i]);
+        Py_XDECREF(n);
+    }
+    Py_DECREF(shape);
+    return ok && o != Py_None && read_pointer(o, out);
 }
 
 // (ctx, layer_begin, layer_count, seq_ids, n_new, k, v, stream)
@@ -141,6 +169,45 @@ PyObject* append_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
         !n_new.read(a[4]) || !read_pointer(a[5], &k) || !read_pointer(a[6], &v) || !read_stream(a[7], &stream))
         return nullptr;
     return call([&] { return tb_append_kv((tb_ctx*)ctx, lb, lc, ids.data, n_new.data, (int32_t)n_new.n, k, v, stream); });
+}
+
+// (ctx, layer_begin, layer_count, seq_ids, pos_begin, pos_end, k_out, v_out, stream)
+PyObject* read_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void *ctx, *k, *v, *stream;
+    int32_t lb, lc;
+    IntList ids, pb, pe;
+    if (!want(n, 9) || !read_address(a[0], &ctx) || !read_int(a[1], &lb) || !read_int(a[2], &lc) || !ids.read(a[3]) || !pb.read(a[4]) ||
+        !pe.read(a[5]) || !read_pointer(a[6], &k) || !read_pointer(a[7], &v) || !read_stream(a[8], &stream))
+        return nullptr;
+    if (!same_length(ids, pb) || !same_length(pe, pb)) return nullptr;
+    return call([&] { return tb_read_kv((tb_ctx*)ctx, lb, lc, ids.data, pb.data, pe.data, (int32_t)pb.n, k, v, stream); });
+}
+
+// (ctx, src_seq, dst_seqs, n_tokens, stream)
+PyObject* fork_sequence(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void *ctx, *stream;
+    int32_t src, n_tokens;
+    IntList dst;
+    if (!want(n, 5) || !read_address(a[0], &ctx) || !read_int(a[1], &src) || !dst.read(a[2]) || !read_int(a[3], &n_tokens) ||
+        !read_stream(a[4], &stream))
+        return nullptr;
+    return call([&] { return tb_fork_sequence((tb_ctx*)ctx, src, dst.data, (int32_t)dst.n, n_tokens, stream); });
+}
+
+// (ctx, seq_ids, keep_begin, n_keep, keep_idx, stream)
+PyObject* compact_sequences(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void *ctx, *idx = nullptr, *stream;
+    int32_t rows = 0, stride = 0;
+    IntList ids, begin, keep;
+    if (!want(n, 6) || !read_address(a[0], &ctx) || !ids.read(a[1]) || !begin.read(a[2]) || !keep.read(a[3]) ||
+        (a[4] != Py_None && !read_matrix(a[4], &idx, &rows, &stride)) || !read_stream(a[5], &stream))
+        return nullptr;
+    if (!same_length(ids, begin) || !same_length(keep, begin)) return nullptr;
+    if (idx && rows < (int32_t)begin.n) {
+        PyErr_SetString(PyExc_ValueError, "a row of positions per sequence is expected");
+        return nullptr;
+    }
+    return call([&] { return tb_compact_sequences((tb_ctx*)ctx, ids.data, (int32_t)begin.n, begin.data, keep.data, (const int32_t*)idx, stride, stream); });
 }
 
 // (ctx, layer_begin, layer_count, seq_ids, pos_begin, pos_end, n_seq, stream)
@@ -188,27 +255,6 @@ PyObject* sparse_decode_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// A tensor (or whatever else has a shape and says where it is) and its leading sizes; `cols` may be null.
-bool read_matrix(PyObject* o, void** out, int32_t* rows, int32_t* cols) {
-    int32_t* sizes[2] = {rows, cols};
-    if (THPVariable_Check(o) && THPVariable_Unpack(o).dim() >= (cols ? 2 : 1)) {
-        const at::Tensor& t = THPVariable_Unpack(o);
-        *out = t.data_ptr();
-        for (int i = 0; i < (cols ? 2 : 1); ++i) *sizes[i] = (int32_t)t.size(i);
-        return true;
-    }
-    PyObject* shape = PyObject_GetAttr(o, g_shape);
-    if (!shape) return false;
-    bool ok = true;
-    for (int i = 0; i < (cols ? 2 : 1) && ok; ++i) {
-        PyObject* n = PySequence_GetItem(shape, i);    // (an IndexError where there are fewer)
-        ok = n && read_int(n, sizes[i]);
-        Py_XDECREF(n);
-    }
-    Py_DECREF(shape);
-    return ok && o != Py_None && read_pointer(o, out);
-}
-
 // (dtype, n_q_heads, n_slots, imp_dim, activation, ln_eps, ln_weight, ln_bias, w1, w2, hidden, scratch, q_imp, stream)
 PyObject* predict_importance_queries(PyObject*, PyObject* const* a, Py_ssize_t n) {
     tb_predictor p;
@@ -236,7 +282,7 @@ PyObject* guarded(PyObject* self, PyObject* const* a, Py_ssize_t n) {
 }
 
 #define TB_METHOD(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {TB_METHOD(append_kv), TB_METHOD(project_keys), TB_METHOD(select_topk), TB_METHOD(sparse_decode_attention),
+PyMethodDef methods[] = {TB_METHOD(append_kv), TB_METHOD(read_kv), TB_METHOD(fork_sequence), TB_METHOD(compact_sequences), TB_METHOD(project_keys), TB_METHOD(select_topk), TB_METHOD(sparse_decode_attention),
                          TB_METHOD(predict_importance_queries), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tokenbutler", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,0 +1,172 @@
+// Cached sequences as wholes: copying one into other slots (parallel samples, beams, a shared prompt) and dropping tokens of one in
+// place (rejected drafts, a branch that keeps part of its context).  Rows are moved as bytes, whatever their type.
+#include "tb_common.cuh"
+#include "tb_internal.h"
+
+namespace tb {
+
+namespace {
+
+// The streams of rows that a (layer, sequence) holds: one per KV head in the K|V cache, then one per head of the projected keys.
+struct RowStream {
+    uint4* base;          // of the cache's first unit
+    int heads, h, chunks; // units per (layer, sequence); this one; 16-byte chunks of a row
+    __device__ __forceinline__ RowStream(const Geom& gm, void* kv, void* kimp, int stream) {
+        const bool rows = stream < gm.Hkv;
+        base = reinterpret_cast<uint4*>(rows ? kv : kimp);
+        heads = rows ? gm.Hkv : gm.Hi, h = rows ? stream : stream - gm.Hkv;
+        chunks = (rows ? gm.row_bytes : gm.dp * (gm.dtype == TB_BF16 ? 2 : 4)) / 16;
+    }
+    __device__ __forceinline__ uint4* unit(const Geom& gm, int layer, int seq) const {
+        return base + (((size_t)layer * gm.max_batch + seq) * heads + h) * gm.max_seq_len * chunks;
+    }
+};
+
+}  // namespace
+
+// A unit's rows are contiguous, so a copy is one run of bytes per unit, read once and written to every slot.
+constexpr int kForkThreads = 256;
+constexpr int kForkUnroll = 4;
+
+__global__ void __launch_bounds__(kForkThreads) fork_kernel(Geom gm, UnitTable ut, ForkArgs a, void* __restrict__ kv, void* __restrict__ kimp,
+                                                            int32_t* __restrict__ lists, int32_t* __restrict__ counts,
+                                                            int32_t* __restrict__ len_dev, int32_t* __restrict__ len_proj_dev,
+                                                            uint32_t* __restrict__ counter) {
+    const int layer = ut.layer_begin + blockIdx.z, stream = blockIdx.y;
+    int n = unit_len(gm, ut, blockIdx.z, 0);
+    if (a.n_tokens >= 0) n = min(n, a.n_tokens);
+    if (stream < gm.Hkv + gm.Hi) {
+        const RowStream rs(gm, kv, kimp, stream);
+        const uint4* src = rs.unit(gm, layer, a.src);
+        const size_t total = (size_t)n * rs.chunks, step = (size_t)gridDim.x * kForkThreads * kForkUnroll;
+        for (size_t at = (size_t)blockIdx.x * kForkThreads * kForkUnroll + threadIdx.x; at < total; at += step) {
+            uint4 v[kForkUnroll];
+#pragma unroll
+            for (int i = 0; i < kForkUnroll; ++i)
+                if (at + i * kForkThreads < total) v[i] = src[at + i * kForkThreads];
+            for (int d = 0; d < a.n_dst; ++d) {
+                uint4* dst = rs.unit(gm, layer, a.dst[d]);
+#pragma unroll
+                for (int i = 0; i < kForkUnroll; ++i)
+                    if (at + i * kForkThreads < total) dst[at + i * kForkThreads] = v[i];
+            }
+        }
+    } else if (a.n_tokens < 0) {                       // the stored lists
+        const size_t unit = ((size_t)layer * gm.max_batch + a.src) * gm.Hl;
+        for (int h = blockIdx.x; h < gm.Hl; h += gridDim.x) {
+            const int cnt = counts[unit + h], m = max(0, min(cnt, gm.idx_cap));
+            for (int d = 0; d < a.n_dst; ++d) {
+                const size_t to = ((size_t)layer * gm.max_batch + a.dst[d]) * gm.Hl + h;
+                for (int i = threadIdx.x; i < m; i += kForkThreads) lists[to * gm.idx_cap + i] = lists[(unit + h) * gm.idx_cap + i];
+                if (threadIdx.x == 0) counts[to] = cnt;
+            }
+        }
+    }
+    if (!ut.use_dev_len || !last_block_arrives(counter, gridDim.x * gridDim.y * gridDim.z)) return;
+    for (int i = threadIdx.x; i < ut.layer_count * a.n_dst; i += kForkThreads) {
+        const size_t row = (size_t)(ut.layer_begin + i / a.n_dst) * gm.max_batch;
+        const int L = len_dev[row + a.src], P = len_proj_dev[row + a.src], most = a.n_tokens < 0 ? L : min(L, a.n_tokens);
+        len_dev[row + a.dst[i % a.n_dst]] = most, len_proj_dev[row + a.dst[i % a.n_dst]] = min(P, most);
+    }
+}
+
+cudaError_t launch_fork(const tb_ctx* c, const UnitTable& ut, const ForkArgs& a, cudaStream_t s) {
+    const Geom& gm = c->geom;
+    const int streams = gm.Hkv + gm.Hi + (a.n_tokens < 0 ? 1 : 0);
+    const long long chunks = (long long)a.max_tokens * (gm.row_bytes / 16);
+    long long bx = (chunks + kForkThreads * kForkUnroll - 1) / (kForkThreads * kForkUnroll);
+    const long long most = 16LL * c->sm_count / (streams * ut.layer_count) + 1;      // a couple of waves of the chip
+    bx = bx < 1 ? 1 : bx > most ? most : bx;
+    dim3 grid((unsigned)bx, streams, ut.layer_count);
+    fork_kernel<<<grid, kForkThreads, 0, s>>>(gm, ut, a, c->kv, c->kimp, c->st.idx, c->st.cnt, c->st.len, c->st.len_proj, c->st.misc_counter + 2);
+    return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Row begin + j becomes row keep[j], in place.  Kept positions ascend, so keep[j] >= begin + j: a row only ever moves down,
+// onto rows that are read with it or were read before it.  A block takes one unit's rows in order, a tile at a time: all threads
+// have read tile t (and, behind the barrier, know it) before any writes it, and what tile t writes lies below all that later tiles
+// read.  Entries that do not ascend or lie outside [begin, length) are reported and their rows left alone (the order above holds for
+// any entry >= begin + j, and others are not followed).
+constexpr int kCompactThreads = 256;
+constexpr int kCompactUnroll = 4;
+
+__global__ void __launch_bounds__(kCompactThreads) compact_kernel(Geom gm, UnitTable ut, CompactArgs a, void* __restrict__ kv, void* __restrict__ kimp,
+                                                                  int32_t* __restrict__ len_dev, int32_t* __restrict__ len_proj_dev,
+                                                                  uint32_t* __restrict__ counter, int32_t* __restrict__ status) {
+    const int ll = blockIdx.z / ut.n_seq, s = blockIdx.z % ut.n_seq, stream = blockIdx.y;
+    const RowStream rs(gm, kv, kimp, stream);
+    const int begin = a.begin[s], L = unit_len(gm, ut, ll, s);
+    // (lengths read on the device may be shorter than the host knew: then nothing is moved and the sequence keeps its length)
+    const int n = begin + a.n_keep[s] <= L ? a.n_keep[s] : 0;
+    uint4* unit = rs.unit(gm, ut.layer_begin + ll, ut.seq_id[s]);
+    const int32_t* keep = a.keep + (size_t)s * a.stride;
+    const int rows = kCompactThreads * kCompactUnroll / rs.chunks;    // of a tile
+    bool bad = begin + a.n_keep[s] > L;
+    for (int j0 = 0; j0 < n; j0 += rows) {
+        uint4 v[kCompactUnroll];
+        int to[kCompactUnroll];
+#pragma unroll
+        for (int i = 0; i < kCompactUnroll; ++i) {
+            const int item = threadIdx.x + i * kCompactThreads, row = item / rs.chunks, j = j0 + row;
+            to[i] = -1;
+            if (row < rows && j < n) {
+                const int t = keep[j];
+                const bool ok = t >= begin + j && t < L && (j == 0 || keep[j - 1] < t);
+                bad |= !ok;
+                if (ok && t > begin + j) {
+                    to[i] = begin + j;
+                    v[i] = unit[(size_t)t * rs.chunks + (item - row * rs.chunks)];
+                }
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kCompactUnroll; ++i) {
+            const int item = threadIdx.x + i * kCompactThreads, row = item / rs.chunks;
+            if (to[i] >= 0) unit[(size_t)to[i] * rs.chunks + (item - row * rs.chunks)] = v[i];
+        }
+    }
+    if (bad) atomicExch(status, kStatusBadIndex);
+    if (!ut.use_dev_len || !last_block_arrives(counter, gridDim.x * gridDim.y * gridDim.z)) return;
+    for (int i = threadIdx.x; i < ut.layer_count * ut.n_seq; i += kCompactThreads) {
+        const int s2 = i % ut.n_seq, want = a.begin[s2] + a.n_keep[s2];
+        const size_t pair = (size_t)(ut.layer_begin + i / ut.n_seq) * gm.max_batch + ut.seq_id[s2];
+        const int len = min(len_dev[pair], want);
+        len_dev[pair] = len;
+        if (len_proj_dev[pair] > len) len_proj_dev[pair] = len;
+    }
+}
+
+cudaError_t launch_compact(const tb_ctx* c, const UnitTable& ut, const CompactArgs& a, cudaStream_t s) {
+    const Geom& gm = c->geom;
+    dim3 grid(1, gm.Hkv + gm.Hi, ut.layer_count * ut.n_seq);
+    compact_kernel<<<grid, kCompactThreads, 0, s>>>(gm, ut, a, c->kv, c->kimp, c->st.len, c->st.len_proj, c->st.misc_counter + 3, c->st.status);
+    return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------------------------------------
+// Resident rows (offloaded KV) of sequences whose rows have moved: the first res_sinks tokens and the res_window most recent ones.
+__global__ void __launch_bounds__(256) refresh_resident_kernel(Geom gm, UnitTable ut, const uint4* __restrict__ kv, uint4* __restrict__ res, int sinks, int window) {
+    const int ll = blockIdx.z / ut.n_seq, s = blockIdx.z % ut.n_seq, chunks = gm.row_bytes / 16;
+    const int L = unit_len(gm, ut, ll, s);
+    const size_t unit = (((size_t)(ut.layer_begin + ll) * gm.max_batch + ut.seq_id[s]) * gm.Hkv + blockIdx.y);
+    const int n_sink = min(sinks, L), w_begin = max(n_sink, L - window), n = n_sink + L - w_begin;
+    const uint4* src = kv + unit * gm.max_seq_len * chunks;
+    uint4* dst = res + unit * (size_t)(sinks + window) * chunks;
+    for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < (long long)n * chunks; i += (long long)gridDim.x * blockDim.x) {
+        const int row = (int)(i / chunks), t = row < n_sink ? row : w_begin + row - n_sink;
+        const int slot = t < sinks ? t : sinks + t % window;
+        dst[(size_t)slot * chunks + i % chunks] = src[(size_t)t * chunks + i % chunks];
+    }
+}
+
+cudaError_t launch_refresh_resident(const tb_ctx* c, const UnitTable& ut, cudaStream_t s) {
+    const Geom& gm = c->geom;
+    const long long chunks = ((long long)c->res_sinks + c->res_window) * (gm.row_bytes / 16);
+    dim3 grid((unsigned)(chunks < 256 * 64 ? (chunks + 255) / 256 : 64), gm.Hkv, ut.layer_count * ut.n_seq);
+    refresh_resident_kernel<<<grid, 256, 0, s>>>(gm, ut, (const uint4*)c->kv, (uint4*)c->res_rows, c->res_sinks, c->res_window);
+    return cudaGetLastError();
+}
+
+}  // namespace tb
