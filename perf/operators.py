@@ -243,6 +243,7 @@ def prepare(case, seed):
             s.ctx.append_kv(0, layers, None, i.new, i.k_new, i.v_new)
         if c["kind"] == "attend":
             s.params = tb.select_params(c["budget"], c["sinks"], c["recent"])
+        s.seen = _seen(s)
     else:
         s.kv = torch.zeros(layers, slots, heads, room, ROW, dtype=torch.uint8, device="cuda") if fp4 else \
             torch.zeros(layers, slots, heads, room, 2, HEAD_DIM, dtype=_values(c), device="cuda")
@@ -285,19 +286,32 @@ def _run_own(s):
         return {"k": s.k_out, "v": s.v_out}
     if kind == "project":
         s.ctx.project_keys(0, c["layers"], None, s.cached, s.ends)
-        return [s.kimp[:, b, :, lo:hi] for b, (lo, hi) in enumerate(zip(s.cached, s.ends))]
+        return s.seen
     if kind == "fork":
         s.ctx.fork_sequence(0, list(range(1, 1 + c["copies"])), s.n_fork)
-        return {"kv": s.kv[:, 1:, :, :s.n_fork], "kimp": s.kimp[:, 1:, :, :s.n_fork]}
+        return s.seen
     if kind == "verify":
         s.ctx.compact_sequences(None, s.cached)
         s.ctx.append_kv(0, c["layers"], None, s.new, s.k_new, s.v_new)
         s.ctx.project_keys(0, c["layers"], None, s.cached, [a + n for a, n in zip(s.cached, s.new)])
         s.ctx.compact_sequences(None, s.cached, s.kept, s.keep)
-        return _kept_rows(s)
+        return s.seen
     s.ctx.fork_sequence(0, [1])
     s.ctx.compact_sequences([1], s.begin, s.kept, s.keep)
-    return {"kv": s.kv[:, 1, :, :s.begin[0] + s.kept[0]], "kimp": s.kimp[:, 1, :, :s.begin[0] + s.kept[0]]}
+    return s.seen
+
+
+def _seen(s):
+    """The parts of the context's caches that a call writes: a program looks at them where they are."""
+    c = s.c
+    if c["kind"] == "project":
+        return [s.kimp[:, b, :, lo:hi] for b, (lo, hi) in enumerate(zip(s.cached, s.ends))]
+    if c["kind"] == "fork":
+        return {"kv": s.kv[:, 1:, :, :s.n_fork], "kimp": s.kimp[:, 1:, :, :s.n_fork]}
+    if c["kind"] == "verify":
+        return _kept_rows(s)
+    if c["kind"] == "prune":
+        return {"kv": s.kv[:, 1, :, :s.begin[0] + s.kept[0]], "kimp": s.kimp[:, 1, :, :s.begin[0] + s.kept[0]]}
 
 
 def _kept_rows(s):
