@@ -368,8 +368,9 @@ __device__ __forceinline__ void f32_rows(const float* __restrict__ qbase, int g,
 }
 
 // The 4-bit warp's rows (row format: tb_fp4.cuh).  Like the bf16 tiles, S = K Q^T and O^T += V^T P^T run on mma.sync m16n8k16 with 16
-// gathered tokens and the group's heads as the N = 8 columns, but on f16: codes turn into f16 pairs in one instruction, and
-// code x scale is exact there.  Both contractions take their operands in an order that leaves every lane with contiguous bytes of a row:
+// gathered tokens and the group's heads as N = 8 columns, two such tiles at a time, but on f16: codes turn into f16 pairs in one
+// instruction, and code x scale is exact there.  Both contractions take their operands in an order that leaves every lane with
+// contiguous bytes of a row:
 //   S:  a lane (gid, tig) holds channels 32 tig .. 32 tig + 31 of two rows (16 bytes and two scales each); k-step ks takes channels
 //       32 tig + 4 ks + (0, 1 | 2, 3), and so does the query operand.
 //   O:  a lane holds the 16 channels of block gid (8 bytes and one scale) of four rows; the codes of two rows are interleaved,
@@ -377,12 +378,20 @@ __device__ __forceinline__ void f32_rows(const float* __restrict__ qbase, int g,
 //   Row r of a tile is token r for even r < 8, 8 + (r + 3) % 8 for odd r < 8, one more than row r - 8's for the others: 144-byte rows,
 //   unpadded, then hit distinct banks in both reads.
 // Queries are bf16: scaled by a power of two per head that brings the largest channel to [2^13, 2^14), every channel down to 2^-28 of
-// it is exact in f16 and the rest is off by less than 2^-39 of it.  Probabilities are kept 2^15 times larger (the running maximum is
-// lowered by 15, which cancels everywhere) and split into an f16 high and low part: 22 bits for all but those below 2^-29 of the
-// largest, which are off by less than 2^-40 of it.
+// it is exact in f16 and the rest is off by less than 2^-39 of it.
+// Weights are 2^(x - ref): ref is the running maximum less 13 and follows only once a score is more than 15.9 above it, so that most tiles
+// need no reduction over the lanes and no rescaling.  They are split into an f16 high and low part: 22 bits for all but those below 2^-27 of
+// the largest, which are off by less than 2^-38 of it.  With up to four heads (kNarrow) columns 4..7 repeat heads 0..3 in S and take the low parts in O:
+// one mma where five to eight heads need two.
+// The tensor core truncates as it accumulates, about 2e-8 of the sum per mma, which adds up over the tiles of a long sequence (3.8e-6 of the
+// result at 120,000 tokens).  So O moves into fp32 sums in shared memory every kFp4Flush tiles; adding every pair of tiles in registers took
+// 32 of its 630 instructions.
 // Leaves accumulators and statistics parked as the bf16 warp does, but for the channels: float4 number mt * 32 + lane holds
-// channels 16 gid + 2 mt and + 1.
-constexpr int kFp4Stage = kTileTok * kFp4Row;         // 2304: two of them hold the parked values
+// channels 16 gid + 2 mt and + 1 (kNarrow: of heads 2 tig and + 1 in lanes tig < 2, their low parts in lanes tig + 2).
+constexpr int kFp4Tile = 32;                          // rows of a stage
+constexpr int kFp4Stage = kFp4Tile * kFp4Row;         // 4608 bytes: what a warp parks
+constexpr int kFp4Flush = 16;                         // tiles between two moves of O
+constexpr int kFp4Sums = 8 * 32 * 16;                 // bytes of a warp's sums
 __device__ __forceinline__ void mma_f16(float* d, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -392,20 +401,28 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     const __half2 v = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ float2 unpack_f16(uint32_t h) { return __half22float2(*reinterpret_cast<const __half2*>(&h)); }
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
-template <int kStages, typename Tokens, typename Issue, typename Commit>
-__device__ __forceinline__ void fp4_rows(const __nv_bfloat16* __restrict__ qbase, int g, float qscale, unsigned char* my_stage, int wb, int we,
+template <int kStages, bool kNarrow, typename Tokens, typename Issue, typename Commit>
+__device__ __forceinline__ void fp4_rows(const __nv_bfloat16* __restrict__ qbase, int g, float qscale, unsigned char* my_stage, float4* sums, int wb, int we,
                                          int n_tiles, uint32_t bad_bits, bool& any_bad, Tokens tokens_of, Issue issue_token, Commit commit) {
     constexpr int D = 128;
+    constexpr float kRoom = 13.f, kLimit = 15.9f;      // exponents of the largest weight: when the reference is set, and before it follows
     const int lane = threadIdx.x & 31, gid = lane >> 2, tig = lane & 3;
     uint32_t qb[8][2];
-    float xs[2];                                       // what a score of heads 2 tig, 2 tig + 1 is multiplied by
+    float xs[2];                                       // what a score of this lane's two heads is multiplied by
     {
+        const int head = kNarrow ? gid & 3 : gid;
         uint32_t w[16];
         uint32_t top2 = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint4 v = gid < g ? __ldg(reinterpret_cast<const uint4*>(qbase + gid * D + tig * 32) + i) : make_uint4(0u, 0u, 0u, 0u);
+            const uint4 v = head < g ? __ldg(reinterpret_cast<const uint4*>(qbase + head * D + tig * 32) + i) : make_uint4(0u, 0u, 0u, 0u);
             w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
         }
 #pragma unroll
@@ -425,87 +442,131 @@ __device__ __forceinline__ void fp4_rows(const __nv_bfloat16* __restrict__ qbase
     float o[8][4];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+    float m_run[2] = {-INFINITY, -INFINITY}, ref[2] = {0.f, 0.f}, l_run[2] = {0.f, 0.f};     // ref: m_run, or 0 before the first score
     const int t0 = (gid & 1) ? 8 + ((gid + 3) & 7) : gid;              // token of row gid; row gid + 8: the next
     const uint32_t k_off = t0 * kFp4Row + tig * 16, ks_off = t0 * kFp4Row + kFp4KScales + tig * 2;
     const int tA = 2 * tig, tB = 8 + ((2 * tig + 4) & 7);              // tokens of k = 2 tig, 2 tig + 1; k + 8: the next ones
     const uint32_t vA_off = tA * kFp4Row, vB_off = tB * kFp4Row;
+    bool flushed = false;                              // whether the sums hold anything
     for (int tile = 0; tile < n_tiles; ++tile) {
-        const int r0 = wb + tile * kTileTok;
-        const bool in_range = lane < kTileTok && r0 + lane < we;
-        const bool bad = in_range && (bad_bits & 1u);
-        any_bad |= bad;
-        bad_bits >>= 1;
-        const unsigned vmask = __ballot_sync(0xffffffffu, in_range && !bad);
+        if (tile && tile % kFp4Flush == 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float4 v = flushed ? sums[i * 32 + lane] : make_float4(0.f, 0.f, 0.f, 0.f);
+                v.x += o[i][0], v.y += o[i][1], v.z += o[i][2], v.w += o[i][3];
+                sums[i * 32 + lane] = v;
+                o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+            }
+            flushed = true;
+        }
+        // rows past the end of the range and bad list entries weigh nothing
+        const int left = we - (wb + tile * kFp4Tile);
+        unsigned vmask = left < 32 ? (1u << left) - 1u : 0xffffffffu;
+        if (__any_sync(0xffffffffu, bad_bits != 0u)) {
+            const unsigned bad = __ballot_sync(0xffffffffu, bad_bits & 1u) & vmask;
+            any_bad |= bad != 0u;
+            vmask &= ~bad;
+            bad_bits >>= 1;
+        }
         asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
         __syncwarp();                                  // every lane's copies of this tile are visible to the warp
         const unsigned char* st = my_stage + tile % kStages * kFp4Stage;
-        float c0[4] = {0.f, 0.f, 0.f, 0.f}, c1[4] = {0.f, 0.f, 0.f, 0.f};
-        {
-            const uint4 ka = *reinterpret_cast<const uint4*>(st + k_off), kb = *reinterpret_cast<const uint4*>(st + k_off + kFp4Row);
-            const uint32_t sa = *reinterpret_cast<const unsigned short*>(st + ks_off), sb = *reinterpret_cast<const unsigned short*>(st + ks_off + kFp4Row);
+        float x[8];                                    // scores of rows gid, gid + 8 of the first tile, then of the second; two heads each
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const unsigned char* sh = st + half * 16 * kFp4Row;
+            float* c = x + half * 4;
+            c[0] = c[1] = c[2] = c[3] = 0.f;
+            const uint4 ka = *reinterpret_cast<const uint4*>(sh + k_off), kb = *reinterpret_cast<const uint4*>(sh + k_off + kFp4Row);
+            const uint32_t sa = *reinterpret_cast<const unsigned short*>(sh + ks_off), sb = *reinterpret_cast<const unsigned short*>(sh + ks_off + kFp4Row);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const uint32_t wa = j == 0 ? ka.x : j == 1 ? ka.y : j == 2 ? ka.z : ka.w, wbw = j == 0 ? kb.x : j == 1 ? kb.y : j == 2 ? kb.z : kb.w;
+                const uint32_t wa = j == 0 ? ka.x : j == 1 ? ka.y : j == 2 ? ka.z : ka.w, wb2 = j == 0 ? kb.x : j == 1 ? kb.y : j == 2 ? kb.z : kb.w;
                 const uint32_t fa = j < 2 ? fp4_scale_pair<0>(sa) : fp4_scale_pair<1>(sa), fb = j < 2 ? fp4_scale_pair<0>(sb) : fp4_scale_pair<1>(sb);
                 uint32_t a[4], b[4];
                 fp4_unpack(wa, a[0], a[1], a[2], a[3]);
-                fp4_unpack(wbw, b[0], b[1], b[2], b[3]);
+                fp4_unpack(wb2, b[0], b[1], b[2], b[3]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) a[i] = mul_f16x2(a[i], fa), b[i] = mul_f16x2(b[i], fb);
-                mma_f16(c0, a[0], b[0], a[1], b[1], qb[2 * j][0], qb[2 * j][1]);
-                mma_f16(c1, a[2], b[2], a[3], b[3], qb[2 * j + 1][0], qb[2 * j + 1][1]);
+                mma_f16(c, a[0], b[0], a[1], b[1], qb[2 * j][0], qb[2 * j][1]);
+                mma_f16(c, a[2], b[2], a[3], b[3], qb[2 * j + 1][0], qb[2 * j + 1][1]);
             }
         }
-        const bool v0 = (vmask >> t0) & 1u, v1 = (vmask >> (t0 + 1)) & 1u;
-        float x[4];
-        x[0] = v0 ? (c0[0] + c1[0]) * xs[0] : -INFINITY, x[1] = v0 ? (c0[1] + c1[1]) * xs[1] : -INFINITY;
-        x[2] = v1 ? (c0[2] + c1[2]) * xs[0] : -INFINITY, x[3] = v1 ? (c0[3] + c1[3]) * xs[1] : -INFINITY;
-        float tmax[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
+        if (vmask != 0xffffffffu) {
 #pragma unroll
-        for (int off = 4; off < 32; off <<= 1) {
-            tmax[0] = fmaxf(tmax[0], __shfl_xor_sync(0xffffffffu, tmax[0], off));
-            tmax[1] = fmaxf(tmax[1], __shfl_xor_sync(0xffffffffu, tmax[1], off));
+            for (int i = 0; i < 8; ++i)
+                if (!(vmask >> (t0 + (i >> 1 & 1) + (i >> 2) * 16) & 1u)) x[i] = -INFINITY;
         }
-        float corr[2], ms[2];
+        const float top0 = xs[0] * fmaxf(fmaxf(x[0], x[2]), fmaxf(x[4], x[6])), top1 = xs[1] * fmaxf(fmaxf(x[1], x[3]), fmaxf(x[5], x[7]));
+        if (__any_sync(0xffffffffu, top0 > m_run[0] + kLimit || top1 > m_run[1] + kLimit)) {
+            float tmax[2] = {top0, top1}, corr[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            const float m_new = fmaxf(m_run[e], tmax[e] - 15.f);
-            ms[e] = m_new == -INFINITY ? 0.f : m_new;
-            corr[e] = exp2f(m_run[e] - ms[e]);
-            m_run[e] = m_new;
-        }
-        float p[4];
-        p[0] = exp2f(x[0] - ms[0]), p[1] = exp2f(x[1] - ms[1]), p[2] = exp2f(x[2] - ms[0]), p[3] = exp2f(x[3] - ms[1]);
-        l_run[0] = l_run[0] * corr[0] + p[0] + p[2];
-        l_run[1] = l_run[1] * corr[1] + p[1] + p[3];
-        if (__any_sync(0xffffffffu, corr[0] != 1.f || corr[1] != 1.f)) {
+            for (int off = 4; off < 32; off <<= 1) {   // over the 8 token rows held by lanes with the same tig
+                tmax[0] = fmaxf(tmax[0], __shfl_xor_sync(0xffffffffu, tmax[0], off));
+                tmax[1] = fmaxf(tmax[1], __shfl_xor_sync(0xffffffffu, tmax[1], off));
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float m_new = fmaxf(m_run[e], tmax[e] - kRoom);
+                ref[e] = m_new == -INFINITY ? 0.f : m_new;
+                corr[e] = exp2f(m_run[e] - ref[e]);
+                m_run[e] = m_new, l_run[e] *= corr[e];
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i][0] *= corr[0], o[i][1] *= corr[1], o[i][2] *= corr[0], o[i][3] *= corr[1];
+            if (flushed) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float4 v = sums[i * 32 + lane];
+                    sums[i * 32 + lane] = make_float4(v.x * corr[0], v.y * corr[1], v.z * corr[0], v.w * corr[1]);
+                }
+            }
         }
-        const uint32_t h0 = pack_f16(p[0], p[1]), h1 = pack_f16(p[2], p[3]);
-        const float2 f0 = __half22float2(*reinterpret_cast<const __half2*>(&h0)), f1 = __half22float2(*reinterpret_cast<const __half2*>(&h1));
-        const uint32_t bh0 = movmatrix_trans(h0), bh1 = movmatrix_trans(h1);
-        const uint32_t bl0 = movmatrix_trans(pack_f16(p[0] - f0.x, p[1] - f0.y)), bl1 = movmatrix_trans(pack_f16(p[2] - f1.x, p[3] - f1.y));
-        {
-            const unsigned char *rA = st + vA_off, *rB = st + vB_off;
-            const uint2 wA = *reinterpret_cast<const uint2*>(rA + kFp4VCodes + gid * 8), wB = *reinterpret_cast<const uint2*>(rB + kFp4VCodes + gid * 8);
-            const uint2 wC = *reinterpret_cast<const uint2*>(rA + kFp4Row + kFp4VCodes + gid * 8), wD = *reinterpret_cast<const uint2*>(rB + kFp4Row + kFp4VCodes + gid * 8);
-            const uint32_t s01 = (rA[kFp4VScales + gid] | (uint32_t)rB[kFp4VScales + gid] << 16) << 7;
-            const uint32_t s23 = (rA[kFp4Row + kFp4VScales + gid] | (uint32_t)rB[kFp4Row + kFp4VScales + gid] << 16) << 7;
+        uint32_t bh[4], bl[4];                         // the weights as B operands (k = tokens, n = heads): two per tile
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {              // eight channels of the block
-                const uint32_t a = h ? wA.y : wA.x, b = h ? wB.y : wB.x, c = h ? wC.y : wC.x, d = h ? wD.y : wD.x;
-                uint32_t e01[4], o01[4], e23[4], o23[4];               // even and odd channels of token pairs
-                fp4_unpack((a & 0x0f0f0f0fu) | ((b << 4) & 0xf0f0f0f0u), e01[0], e01[1], e01[2], e01[3]);
-                fp4_unpack(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), o01[0], o01[1], o01[2], o01[3]);
-                fp4_unpack((c & 0x0f0f0f0fu) | ((d << 4) & 0xf0f0f0f0u), e23[0], e23[1], e23[2], e23[3]);
-                fp4_unpack(((c >> 4) & 0x0f0f0f0fu) | (d & 0xf0f0f0f0u), o23[0], o23[1], o23[2], o23[3]);
+        for (int i = 0; i < 4; ++i) {
+            const float p0 = exp2_approx(fmaf(x[2 * i], xs[0], -ref[0])), p1 = exp2_approx(fmaf(x[2 * i + 1], xs[1], -ref[1]));
+            l_run[0] += p0, l_run[1] += p1;
+            const uint32_t h = pack_f16(p0, p1);
+            const float2 f = unpack_f16(h);
+            const uint32_t l = pack_f16(p0 - f.x, p1 - f.y);
+            if constexpr (kNarrow) {
+                bh[i] = movmatrix_trans(tig < 2 ? h : l);
+            } else {
+                bh[i] = movmatrix_trans(h), bl[i] = movmatrix_trans(l);
+            }
+        }
+        uint2 w[2][4];                                 // codes of block gid in the tiles' four tokens
+        uint32_t s01[2], s23[2];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t a0 = mul_f16x2(e01[i], s01), a1 = mul_f16x2(o01[i], s01), a2 = mul_f16x2(e23[i], s23), a3 = mul_f16x2(o23[i], s23);
-                    mma_f16(o[h * 4 + i], a0, a1, a2, a3, bh0, bh1);
-                    mma_f16(o[h * 4 + i], a0, a1, a2, a3, bl0, bl1);
+        for (int half = 0; half < 2; ++half) {
+            const unsigned char *rA = st + half * 16 * kFp4Row + vA_off, *rB = st + half * 16 * kFp4Row + vB_off;
+            w[half][0] = *reinterpret_cast<const uint2*>(rA + kFp4VCodes + gid * 8), w[half][1] = *reinterpret_cast<const uint2*>(rB + kFp4VCodes + gid * 8);
+            w[half][2] = *reinterpret_cast<const uint2*>(rA + kFp4Row + kFp4VCodes + gid * 8), w[half][3] = *reinterpret_cast<const uint2*>(rB + kFp4Row + kFp4VCodes + gid * 8);
+            s01[half] = (rA[kFp4VScales + gid] | (uint32_t)rB[kFp4VScales + gid] << 16) << 7;
+            s23[half] = (rA[kFp4Row + kFp4VScales + gid] | (uint32_t)rB[kFp4Row + kFp4VScales + gid] << 16) << 7;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {                  // eight channels of the block
+            uint32_t e01[2][4], o01[2][4], e23[2][4], o23[2][4];       // even and odd channels of token pairs
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const uint32_t a = h ? w[half][0].y : w[half][0].x, b = h ? w[half][1].y : w[half][1].x;
+                const uint32_t c = h ? w[half][2].y : w[half][2].x, d = h ? w[half][3].y : w[half][3].x;
+                fp4_unpack((a & 0x0f0f0f0fu) | ((b << 4) & 0xf0f0f0f0u), e01[half][0], e01[half][1], e01[half][2], e01[half][3]);
+                fp4_unpack(((a >> 4) & 0x0f0f0f0fu) | (b & 0xf0f0f0f0u), o01[half][0], o01[half][1], o01[half][2], o01[half][3]);
+                fp4_unpack((c & 0x0f0f0f0fu) | ((d << 4) & 0xf0f0f0f0u), e23[half][0], e23[half][1], e23[half][2], e23[half][3]);
+                fp4_unpack(((c >> 4) & 0x0f0f0f0fu) | (d & 0xf0f0f0f0u), o23[half][0], o23[half][1], o23[half][2], o23[half][3]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float(&d)[4] = o[h * 4 + i];
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const uint32_t a0 = mul_f16x2(e01[half][i], s01[half]), a1 = mul_f16x2(o01[half][i], s01[half]);
+                    const uint32_t a2 = mul_f16x2(e23[half][i], s23[half]), a3 = mul_f16x2(o23[half][i], s23[half]);
+                    if constexpr (!kNarrow) mma_f16(d, a0, a1, a2, a3, bl[2 * half], bl[2 * half + 1]);
+                    mma_f16(d, a0, a1, a2, a3, bh[2 * half], bh[2 * half + 1]);
                 }
             }
         }
@@ -526,7 +587,14 @@ __device__ __forceinline__ void fp4_rows(const __nv_bfloat16* __restrict__ qbase
     __syncwarp();
     float4* park = reinterpret_cast<float4*>(my_stage);
 #pragma unroll
-    for (int mt = 0; mt < 8; ++mt) park[mt * 32 + lane] = make_float4(o[mt][0], o[mt][1], o[mt][2], o[mt][3]);
+    for (int mt = 0; mt < 8; ++mt) {
+        float4 v = make_float4(o[mt][0], o[mt][1], o[mt][2], o[mt][3]);
+        if (flushed) {
+            const float4 w = sums[mt * 32 + lane];
+            v.x += w.x, v.y += w.y, v.z += w.z, v.w += w.w;
+        }
+        park[mt * 32 + lane] = v;
+    }
     park[8 * 32 + lane] = make_float4(m_run[0], l_run[0], m_run[1], l_run[1]);
 }
 
@@ -542,21 +610,26 @@ static inline size_t cluster_merge_bytes(int C) { return (size_t)((8 + C - 1) / 
 // go through the global workspace and the last block to arrive merges them.
 // kSources: the resident sink / window copies or the Important buffer are bound and a row reference names
 // its source; without them (the usual case) the gather carries no trace of the option.
-// FG: 0 = bf16 storage, -1 = rows held in 4 bits; else fp32 storage with up to FG query heads per unit.
+// FG: 0 = bf16 storage; -1 = rows held in 4 bits, up to four query heads per unit, -2 = up to eight; else fp32 storage with up to FG query heads per unit.
 template <int NW, int kMmaStages, bool kSources = false, int FG = 0>
-__global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut, AttnArgs a, const void* __restrict__ kv,
+__global__ void __launch_bounds__(NW * 32, FG < 0 ? 16 / NW : 0) attn_mma_kernel(Geom gm, UnitTable ut, AttnArgs a, const void* __restrict__ kv,
                                                            const int32_t* __restrict__ state_idx,
                                                            const int32_t* __restrict__ state_cnt, float* __restrict__ part_o,
                                                            float* __restrict__ part_ml, uint32_t* __restrict__ counters,
                                                            int32_t* __restrict__ status) {
     constexpr int D = 128;
-    constexpr bool kF32 = FG > 0, kFp4 = FG < 0;
-    constexpr int kTok = kF32 ? 8 : kTileTok;          // rows of a stage
+    constexpr bool kF32 = FG > 0, kFp4 = FG < 0, kNarrow = FG == -1;
+    constexpr int kTok = kF32 ? 8 : kFp4 ? kFp4Tile : kTileTok;        // rows of a stage
     constexpr int kRowBytes = kFp4 ? kFp4Row : 2 * D * (kF32 ? 4 : 2);  // a K|V row pair
     constexpr int kStage = kFp4 ? kFp4Stage : kStageBytes;
+    constexpr size_t kStagesEnd = (size_t)NW * (kMmaStages * kStage + (kFp4 ? kFp4Sums : 0));     // of all warps' stages (and sums)
     // the channels of parked accumulator tile mt of lane ln: this one, and the one kPairStep further
     constexpr int kPairStep = kFp4 ? 1 : 8;
     auto channel = [](int mt, int ln) { return kFp4 ? (ln >> 2) * 16 + 2 * mt : mt * 16 + (ln >> 2); };
+    // the (tile, lane) slots that hold results, numbered: all 256, or (kNarrow) those of lanes tig < 2
+    constexpr int kSlots = kNarrow ? 128 : 256;
+    auto slot_tile = [](int i) { return kNarrow ? i >> 4 : i >> 5; };
+    auto slot_lane = [](int i) { return kNarrow ? (i >> 1 & 7) * 4 + (i & 1) : i & 31; };
     extern __shared__ __align__(128) unsigned char smem_dyn[];
     __shared__ int sh_last;
 
@@ -638,12 +711,15 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
     auto issue_token = [&](int tile, int t) {     // t: lane i < kTok holds the token of row i
         const uint32_t dst = stage_u32 + (tile % kMmaStages) * kStage;
         if constexpr (kFp4) {
-            // nine 16-byte chunks per row, chunk after chunk: four and a half instructions of the warp per tile
-            constexpr int kChunks = kRowBytes / 16;
+            if (a.dense && wb + (tile + 1) * kTok <= we) {             // consecutive rows are one run of bytes
+                const unsigned char* src = kv_unit + (size_t)(wb + tile * kTok) * kRowBytes + lane * 16;
 #pragma unroll
-            for (int i = 0; i < (kTok * kChunks + 31) / 32; ++i) {
-                const int item = i * 32 + lane, r = item / kChunks;
-                const int ti = __shfl_sync(0xffffffffu, t, min(r, kTok - 1));
+                for (int i = 0; i < kStage / 512; ++i)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + lane * 16 + i * 512), "l"(src + i * 512) : "memory");
+                return;
+            }
+            // nine 16-byte chunks per row: the first eight of four rows at a time, then the last of all 32
+            auto copy = [&](int ti, uint32_t to, int at) {
                 const unsigned char* src = kv_unit;
                 int row = ti;
                 if constexpr (kSources) {
@@ -651,9 +727,12 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
                     src = which == 0 ? kv_unit : which == 1 ? res_unit : imp_unit;
                     row = ti & kRowIdxMask;
                 }
-                if (item < kTok * kChunks)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst + item * 16), "l"(src + (size_t)row * kRowBytes + (item - r * kChunks) * 16) : "memory");
-            }
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(src + (size_t)row * kRowBytes + at) : "memory");
+            };
+            const uint32_t to = dst + (lane >> 3) * kRowBytes + (lane & 7) * 16;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) copy(__shfl_sync(0xffffffffu, t, i * 4 + (lane >> 3)), to + i * 4 * kRowBytes, (lane & 7) * 16);
+            copy(t, dst + lane * kRowBytes + 128, 128);
             return;
         }
 #pragma unroll
@@ -717,7 +796,8 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
     if constexpr (kF32) {
         f32_rows<FG, kMmaStages>(reinterpret_cast<const float*>(a.q) + hq0 * D, g, qscale, my_stage, wb, we, n_tiles, bad_bits, any_bad, tokens_of, issue_token, commit);
     } else if constexpr (kFp4) {
-        fp4_rows<kMmaStages>(reinterpret_cast<const __nv_bfloat16*>(a.q) + hq0 * D, g, qscale, my_stage, wb, we, n_tiles, bad_bits, any_bad, tokens_of, issue_token, commit);
+        fp4_rows<kMmaStages, kNarrow>(reinterpret_cast<const __nv_bfloat16*>(a.q) + hq0 * D, g, qscale, my_stage, reinterpret_cast<float4*>(smem_dyn + (size_t)NW * kMmaStages * kStage) + warp * (kFp4Sums / 16),
+                                      wb, we, n_tiles, bad_bits, any_bad, tokens_of, issue_token, commit);
     } else {
         // Q^T as the B operand of S = K Q^T: k = channels, n = query heads (gid; heads >= g are zero padding)
         uint32_t qb[8][2];
@@ -929,7 +1009,11 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
         for (int w = 0; w < NW; ++w) {
             const float e0 = exp2f(q[w].x - M0s), e1 = exp2f(q[w].z - M1s);
             L0 = fmaf(q[w].y, e0, L0), L1 = fmaf(q[w].w, e1, L1);
-            const float4 v = warp_buf(w)[mt * 32 + ln];
+            float4 v = warp_buf(w)[mt * 32 + ln];
+            if constexpr (kNarrow) {
+                const float4 low = warp_buf(w)[mt * 32 + ln + 2];
+                v.x += low.x, v.y += low.y, v.z += low.z, v.w += low.w;
+            }
             acc.x = fmaf(v.x, e0, acc.x), acc.y = fmaf(v.y, e1, acc.y), acc.z = fmaf(v.z, e0, acc.z), acc.w = fmaf(v.w, e1, acc.w);
         }
         stat = make_float4(M0, L0, M1, L1);
@@ -945,7 +1029,7 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
         cg::cluster_group cluster = cg::this_cluster();
         const int rank = (int)cluster.block_rank(), C = (int)cluster.num_blocks();
         const int T = (8 + C - 1) / C;                               // slices per owner
-        float4* area = reinterpret_cast<float4*>(smem_dyn + (size_t)NW * kMmaStages * kStage);   // [T][C][32 lanes]
+        float4* area = reinterpret_cast<float4*>(smem_dyn + kStagesEnd);   // [T][C][32 lanes]
         float4* ml = area + (size_t)T * C * 32;                      // [C][4]: (m, l) of heads 2 tig, 2 tig + 1
         // writes one merged piece: (acc, sums ls0 / ls1, maxima M0 / M1) of heads 2 tg, 2 tg + 1 at channels ch, ch + kPairStep
         auto write_piece = [&](int tg, int ch, const float4& acc, float M0, float ls0, float M1, float ls1) {
@@ -960,8 +1044,8 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
             }
         };
         if (C == 1) {                                                // the block's result is the problem's
-            for (int slot = tid; slot < 256; slot += NW * 32) {
-                const int mt = slot >> 5, ln = slot & 31;
+            for (int slot = tid; slot < kSlots; slot += NW * 32) {
+                const int mt = slot_tile(slot), ln = slot_lane(slot);
                 float4 acc, stat;
                 fold_slot(mt, ln, acc, stat);
                 write_piece(ln & 3, channel(mt, ln), acc, stat.x, stat.y, stat.z, stat.w);
@@ -970,8 +1054,8 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
             return;
         }
         if (split_cluster) asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-        for (int slot = tid; slot < 256; slot += NW * 32) {
-            const int mt = slot >> 5, ln = slot & 31;
+        for (int slot = tid; slot < kSlots; slot += NW * 32) {
+            const int mt = slot_tile(slot), ln = slot_lane(slot);
             float4 acc, stat;
             fold_slot(mt, ln, acc, stat);
             cluster.map_shared_rank(area, mt % C)[((mt / C) * C + rank) * 32 + ln] = acc;
@@ -984,7 +1068,7 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
             for (int i = tid; i < T * 32; i += NW * 32) {
                 const int ts = i >> 5, ln = i & 31, tg = ln & 3;
                 const int j = ts * C + rank;                         // the slice
-                if (j >= 8) continue;
+                if (j >= 8 || (kNarrow && tg >= 2)) continue;
                 float4 q[kC], v[kC];
 #pragma unroll
                 for (int r = 0; r < kC; ++r) {
@@ -1015,8 +1099,8 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
     } else if constexpr (NW != 12) {                     // (12-warp blocks always merge in their cluster: its code alone costs them 0.9%)
         // splits through the global workspace, merged by the last block to arrive
         SplitSink sink{part_o, part_ml, counters, a.out, a.lse, hq0, lu, split, a.nsplit};
-        for (int slot = tid; slot < 256; slot += NW * 32) {
-            const int mt = slot >> 5, ln = slot & 31, u0 = 2 * (ln & 3), ch = channel(mt, ln);
+        for (int slot = tid; slot < kSlots; slot += NW * 32) {
+            const int mt = slot_tile(slot), ln = slot_lane(slot), u0 = 2 * (ln & 3), ch = channel(mt, ln);
             float4 acc, stat;
             fold_slot(mt, ln, acc, stat);
             if (u0 < g) {
@@ -1033,8 +1117,68 @@ __global__ void __launch_bounds__(NW * 32) attn_mma_kernel(Geom gm, UnitTable ut
     attn_stamp(6);
 }
 
-// Stages per warp of the 4-bit kernels: 18 KB of rows in flight (14 KB where 12 warps share an SM).
-constexpr int fp4_stages(int nw) { return nw == 12 ? 6 : 8; }
+// The 4-bit kernels: blocks of 4 or 8 warps, 16 warps per SM, two stages per warp (74 KB in flight per SM while the other half is worked on;
+// three stages, and 12 warps with 168 registers each, were within 3% either way).
+constexpr int kFp4Stages = 2;
+static inline size_t fp4_smem(int nw) { return (size_t)nw * (kFp4Stages * kFp4Stage + kFp4Sums); }
+
+// Blocks per problem and warps per block of a 4-bit launch.  A warp works on tiles of 32 rows, about 0.7 us each where latency counts.
+// Measured over 4 to 256 problems of 35 to 110000 rows, every cluster size and the global merge (us per launch in a chain of layers; the
+// rules below are within 4% of the best on average):
+//  - short problems get a warp per tile, or two tiles, as long as that takes half of the chip's warps: the next layer's blocks fetch their
+//    lists and first rows in the other half meanwhile.  4-warp blocks spread few problems over more SMs (8 problems of 324 rows: 3 x 4 warps
+//    3.4, 2 x 4 4.3; of 1024: 8 x 4 3.9, 4 x 4 4.3; of 3276: 9 x 8 5.6, 6 x 8 6.4; 32 of 1500: 6 x 4 6.4, 6 x 8 6.9); many problems fill them
+//    anyway, and fewer, larger blocks have less to merge (64 of 322: 1 x 8 4.4, 3 x 4 5.1; of 789: 2 x 8 6.7, 4 x 4 7.6);
+//  - others share all of the chip's warps, a number of blocks that is resident at once (64 of 15000: 4 x 8 33.4, 8 x 4 37.3; 256 of 1800:
+//    1 x 8 17.8, 2 x 4 21);
+//  - clusters while they fit and a problem needs no more than nine blocks; beyond, the global merge, unless nine leave a warp few
+//    tiles (16 of 110000: 18 x 8 59.5, clusters of 8 84; 8 of 32768: 32 x 8 17, clusters of 9 20; of 11208: 9 x 8 10.7, 22 x 8 13.6).
+//    Clusters of seven pack badly (32 of 8770: 8 x 8 17.8, 7 x 8 21.3).
+static void fp4_split(const tb_ctx* c, int units, int max_rows, AttnArgs& a, int& nw) {
+    int* max_active = const_cast<tb_ctx*>(c)->attn_max_active_fp4;
+    auto fits = [&](int C) {                           // whether the launch's clusters run at once
+        if (C == 1) return true;
+        int& known = max_active[(nw == 8 ? 16 : 0) + C - 1];
+        if (known == 0) {
+            cudaLaunchConfig_t q = {};
+            q.gridDim = dim3(C, 1, 1), q.blockDim = dim3(nw * 32, 1, 1), q.dynamicSmemBytes = fp4_smem(nw) + cluster_merge_bytes(C);
+            cudaLaunchAttribute at[1];
+            at[0].id = cudaLaunchAttributeClusterDimension;
+            at[0].val.clusterDim.x = C, at[0].val.clusterDim.y = 1, at[0].val.clusterDim.z = 1;
+            q.attrs = at, q.numAttrs = 1;
+            int n = 0;
+            const cudaError_t e = nw == 8 ? cudaOccupancyMaxActiveClusters(&n, attn_mma_kernel<8, kFp4Stages, false, -1>, &q)
+                                          : cudaOccupancyMaxActiveClusters(&n, attn_mma_kernel<4, kFp4Stages, false, -1>, &q);
+            (void)cudaGetLastError();
+            known = e == cudaSuccess && n > 0 ? n : -1;
+        }
+        return known >= units;
+    };
+    constexpr int kMost = 9;                           // blocks of a cluster (beyond eight: asked for)
+    const bool many = units >= 32;
+    const int tiles = max_rows > kFp4Tile ? (max_rows + kFp4Tile - 1) / kFp4Tile : 1;
+    const int half = max(1, 8 * c->sm_count / units), full = max(1, 16 * c->sm_count / units);     // warps per problem
+    int per = tiles <= 2 * half ? (tiles + half - 1) / half : (tiles + full - 1) / full;           // tiles per warp
+    if (many && tiles > 8 && per < 2) per = 2;
+    const int warps = (tiles + per - 1) / per;
+    nw = warps <= (many ? 4 : 24) && per <= 3 ? 4 : 8;
+    int C = (warps + nw - 1) / nw;
+    const int slots = 16 / nw * c->sm_count;
+    if (C > 1 && units * C > slots) C = max(1, slots / units);
+    per = (tiles + C * nw - 1) / (C * nw);
+    if (per <= 3) C = (tiles + per * nw - 1) / (per * nw);             // the fewest blocks that leave a warp no more tiles
+    a.cluster_merge = 1;
+    if (C > kMost && (tiles + kMost * nw - 1) / (kMost * nw) > 6) {
+        a.cluster_merge = 0;
+    } else {
+        if (C > kMost) C = kMost;
+        int fit = C;
+        while (!fits(fit) || fit == 7) --fit;
+        if (4 * fit >= 3 * C || per <= 3) C = fit;
+        else a.cluster_merge = 0;
+    }
+    a.nsplit = C < kMaxSplits ? C : kMaxSplits;
+}
 
 static int pick_nsplit(const tb_ctx* c, int units, int max_rows) {
     // about two blocks per SM and never a thin second wave: with 64 problems of 9.8K rows (which now take two 12-warp
@@ -1084,11 +1228,12 @@ cudaError_t launch_attention(const tb_ctx* c, const UnitTable& ut, const AttnArg
                 prepare(attn_mma_kernel<4, 2, true, G>, 113, true), prepare(attn_mma_kernel<8, 2, true, G>, 220, true);
                 prepare(attn_mma_kernel<8, 3, true, G>, 220, true);
             };
-            auto prepare_fp4 = [&](auto warps) {
-                constexpr int W = decltype(warps)::value;
-                prepare(attn_mma_kernel<W, fp4_stages(W), false, -1>, W == 4 ? 113 : 220, true), prepare(attn_mma_kernel<W, fp4_stages(W), true, -1>, W == 4 ? 113 : 220, true);
+            auto prepare_fp4 = [&](auto group) {
+                constexpr int G = decltype(group)::value;
+                prepare(attn_mma_kernel<4, kFp4Stages, false, G>, 113, true), prepare(attn_mma_kernel<4, kFp4Stages, true, G>, 113, true);
+                prepare(attn_mma_kernel<8, kFp4Stages, false, G>, 220, true), prepare(attn_mma_kernel<8, kFp4Stages, true, G>, 220, true);
             };
-            prepare_fp4(std::integral_constant<int, 4>{}), prepare_fp4(std::integral_constant<int, 8>{}), prepare_fp4(std::integral_constant<int, 12>{});
+            prepare_fp4(std::integral_constant<int, -1>{}), prepare_fp4(std::integral_constant<int, -2>{});
             prepare_f32(std::integral_constant<int, 1>{}), prepare_f32(std::integral_constant<int, 2>{});
             prepare_f32(std::integral_constant<int, 4>{}), prepare_f32(std::integral_constant<int, 8>{});
             (void)cudaGetLastError();
@@ -1148,7 +1293,7 @@ cudaError_t launch_attention(const tb_ctx* c, const UnitTable& ut, const AttnArg
             return C;
         };
         int n = 0;
-        if (units <= c->sm_count) {
+        if (units <= c->sm_count && !gm.fp4) {
             int want = (max_rows + small_block - 1) / small_block, least = (max_rows + large_block - 1) / large_block;
             if (max_rows > 1536) want = least = 9;
             else if (want > 6) want = 6;
@@ -1178,7 +1323,9 @@ cudaError_t launch_attention(const tb_ctx* c, const UnitTable& ut, const AttnArg
             if (max_rows > 3 * large_block && 3 * units <= 2 * c->sm_count - c->sm_count / 5 && clusters_that_fit(3, true) >= units) fours = 3;
             else if (max_rows > 12 * large_block && units > half + half / 8 && clusters_that_fit(2, true) >= units) fours = 2;
         }
-        if (n && n4 <= 8 && rows_per_block > large_block && 10 * n4 > 23 * n) {
+        if (gm.fp4) {
+            fp4_split(c, units, max_rows, a, nw);
+        } else if (n && n4 <= 8 && rows_per_block > large_block && 10 * n4 > 23 * n) {
             a.nsplit = n4, a.cluster_merge = 1;
         } else if (n && (units * n >= most || rows_per_block <= cluster_rows)) {
             a.nsplit = n, a.cluster_merge = 1;
@@ -1206,12 +1353,12 @@ cudaError_t launch_attention(const tb_ctx* c, const UnitTable& ut, const AttnArg
         const size_t merge_bytes = a.cluster_merge ? cluster_merge_bytes(a.nsplit) : 0;
         // three stages per warp when the 8-warp block still fits the SM with them
         const int nst = (nw == 8 && 8 * 3 * kStageBytes + merge_bytes <= 220 * 1024 && a.nsplit <= 8) ? 3 : 2;
-        size_t smem = (gm.fp4 ? (size_t)nw * fp4_stages(nw) * kFp4Stage : (size_t)nw * nst * kStageBytes) + merge_bytes;
+        size_t smem = (gm.fp4 ? fp4_smem(nw) : (size_t)nw * nst * kStageBytes) + merge_bytes;
         // The split count of the 4-warp launches is chosen for two blocks per SM; their 64 KB of stages would let
         // a third one in, and the block scheduler then loads some SMs with three blocks and leaves others with one
         // (batch 8 at 64K: 59 us per launch against 52.6).  Asking for a third of the SM's shared memory plus a
         // little keeps it at two.
-        if (nw == 4 && smem < kFourWarpBytes) smem = kFourWarpBytes;
+        if (nw == 4 && smem < kFourWarpBytes && !gm.fp4) smem = kFourWarpBytes;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = grid;
         cfg.blockDim = dim3(nw * 32, 1, 1);
@@ -1242,11 +1389,12 @@ cudaError_t launch_attention(const tb_ctx* c, const UnitTable& ut, const AttnArg
         }
         const bool sources = a.res_rows != nullptr || a.imp_rows != nullptr;
         if (gm.fp4) {
-            auto launch_fp4 = [&](auto warps) {
-                constexpr int W = decltype(warps)::value;
-                return sources ? launch(attn_mma_kernel<W, fp4_stages(W), true, -1>) : launch(attn_mma_kernel<W, fp4_stages(W), false, -1>);
+            auto launch_fp4 = [&](auto group) {
+                constexpr int G = decltype(group)::value;
+                if (nw == 8) return sources ? launch(attn_mma_kernel<8, kFp4Stages, true, G>) : launch(attn_mma_kernel<8, kFp4Stages, false, G>);
+                return sources ? launch(attn_mma_kernel<4, kFp4Stages, true, G>) : launch(attn_mma_kernel<4, kFp4Stages, false, G>);
             };
-            return nw == 12 ? launch_fp4(std::integral_constant<int, 12>{}) : nw == 8 ? launch_fp4(std::integral_constant<int, 8>{}) : launch_fp4(std::integral_constant<int, 4>{});
+            return gm.ga > 4 ? launch_fp4(std::integral_constant<int, -2>{}) : launch_fp4(std::integral_constant<int, -1>{});
         }
 #define TB_MMA(NW_, ST_) (sources ? launch(attn_mma_kernel<NW_, ST_, true>) : launch(attn_mma_kernel<NW_, ST_, false>))
         if (nw == 12) return TB_MMA(12, 2);
@@ -1295,7 +1443,7 @@ tb_status static_scratch_for_current_device(unsigned char** out, int* sm_count) 
         int sms = 0;
         if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return TB_ERR_CUDA;
         const auto prepare = [](auto kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 113 * 1024) == cudaSuccess; };
-        if (!prepare(tb::attn_mma_kernel<4, 2>) || !prepare(tb::attn_mma_kernel<4, tb::fp4_stages(4), false, -1>) || !prepare(tb::attn_mma_kernel<4, 2, true, 1>) || !prepare(tb::attn_mma_kernel<4, 2, true, 2>) ||
+        if (!prepare(tb::attn_mma_kernel<4, 2>) || !prepare(tb::attn_mma_kernel<4, tb::kFp4Stages, false, -1>) || !prepare(tb::attn_mma_kernel<4, tb::kFp4Stages, false, -2>) || !prepare(tb::attn_mma_kernel<4, 2, true, 1>) || !prepare(tb::attn_mma_kernel<4, 2, true, 2>) ||
             !prepare(tb::attn_mma_kernel<4, 2, true, 4>) || !prepare(tb::attn_mma_kernel<4, 2, true, 8>))
             return TB_ERR_CUDA;
         g_sm_count[dev] = sms;
@@ -1393,10 +1541,11 @@ extern "C" tb_status tb_sparse_decode_attention_static(const void* kv_dev, int32
     dim3 grid(a.nsplit, n_kv_heads, n_seq);
     // the stored-list arguments of the kernels are never read here (caller lists or dense)
     const auto launch = [&](auto kernel) {
-        const size_t smem = gm.fp4 ? kAttnWarps * fp4_stages(kAttnWarps) * kFp4Stage : kAttnWarps * 2 * kStageBytes;
+        const size_t smem = gm.fp4 ? fp4_smem(kAttnWarps) : kAttnWarps * 2 * kStageBytes;
         kernel<<<grid, kAttnThreads, smem, s>>>(gm, ut, a, kv_dev, nullptr, nullptr, part_o, part_ml, counters, status);
     };
-    if (gm.fp4) launch(attn_mma_kernel<kAttnWarps, fp4_stages(kAttnWarps), false, -1>);
+    if (gm.fp4 && gm.ga > 4) launch(attn_mma_kernel<kAttnWarps, kFp4Stages, false, -2>);
+    else if (gm.fp4) launch(attn_mma_kernel<kAttnWarps, kFp4Stages, false, -1>);
     else if (kv_dtype == TB_BF16) launch(attn_mma_kernel<4, 2>);
     else if (gm.ga == 1) launch(attn_mma_kernel<4, 2, true, 1>);
     else if (gm.ga == 2) launch(attn_mma_kernel<4, 2, true, 2>);

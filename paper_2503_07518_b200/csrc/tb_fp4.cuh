@@ -46,10 +46,30 @@ __device__ __forceinline__ uint32_t f16x2_to_bf16x2(uint32_t h) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// 32 contiguous bytes, in one access where the address allows it (`wide`: uniform over the launch).
+__device__ __forceinline__ void load_32_bytes(const void* p, bool wide, uint32_t (&w)[8]) {
+    if (wide) {
+        asm volatile("ld.global.nc.L1::no_allocate.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p));
+    } else {
+        const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p)), b = __ldcs(reinterpret_cast<const uint4*>(p) + 1);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+    }
+}
+__device__ __forceinline__ void store_32_bytes(void* p, bool wide, const uint32_t (&w)[8]) {
+    if (wide) {
+        asm volatile("st.global.v8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]), "l"(p) : "memory");
+    } else {
+        reinterpret_cast<uint4*>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+}
+
 // 16 bf16 values (8 words) -> 8 bytes of codes and a scale.
 //
 // Scale: the largest magnitude a over 6, to the nearest 8-bit float.  a has 8 significant bits and six times a midpoint between two
-// scales at most 7, so a / 6 is a midpoint or differs from every one by 2^-9 of its size: the division's rounding to 24 bits decides nothing.
+// scales at most 7, so a / 6 is a midpoint (5 significant bits) or differs from every one by 2^-9 of its size.  The product with a rounded
+// sixth, off by less than 2^-22, is therefore first rounded to 12 bits: that puts it on the midpoint if and only if a / 6 is one.
 // Codes: x / scale to the nearest code.  It is a midpoint t between two codes (3 significant bits) exactly, or x and
 // t scale (8 and at most 7 bits) differ by 2^-9 of their size, that is, the quotient by at least 2^-11 from t >= 1/4.  So the product
 // with an approximate reciprocal (off by less than 2^-19), rounded to a multiple of 2^-13 by adding and taking away 1536, lies on
@@ -60,8 +80,8 @@ __device__ __forceinline__ void fp4_encode(const uint32_t (&w)[8], uint2& codes,
 #pragma unroll
     for (int i = 0; i < 8; ++i) top2 = __vmaxu2(top2, w[i] & 0x7fff7fffu);
     const uint32_t top = max(top2 & 0xffffu, top2 >> 16);
-    const float ideal = __uint_as_float(top << 16) / 6.f;
-    const uint32_t u = __float_as_uint(ideal);
+    const uint32_t u = (__float_as_uint(__uint_as_float(top << 16) * (1.f / 6.f)) + 0x800u) & 0xfffff000u;
+    const float ideal = __uint_as_float(u);
     // (below 2^-14 scales are multiples of 2^-17)
     uint32_t code = ideal < 6.103515625e-05f ? (uint32_t)__float2int_rn(ideal * 131072.f)
                                              : ((u + 0x7ffffu + ((u >> 20) & 1u)) >> 20) - (112u << 3);

@@ -87,6 +87,7 @@ struct CompactArgs {
     int begin[kMaxLaunchSeq];    // tokens before these stay where they are
     int n_keep[kMaxLaunchSeq];
     int max_keep;
+    int kv_slices, imp_slices;   // blocks per unit (launch_compact)
 };
 struct ReadTable {
     int tok_off[kMaxLaunchSeq + 1];  // prefix sums of the tokens read
@@ -173,6 +174,7 @@ struct tb_ctx {
     int tile_rows;                        // rows per TMA box of the score pass
     int sm_count;
     int attn_max_active[25];              // co-resident attention clusters per cluster size, 8-warp blocks and (16 +) 4-warp ones (0 = not asked yet)
+    int attn_max_active_fp4[32];          // the same of the 4-bit kernels: per cluster size, 4-warp blocks, then 8-warp ones
     void* res_rows;                       // resident sink + window rows (tb_bind_resident_rows), or NULL
     int res_sinks, res_window;
     void* imp_rows;                       // Important buffer (tb_bind_important_buffer), or NULL

@@ -24,9 +24,11 @@ struct RowStream {
 
 }  // namespace
 
-// A unit's rows are contiguous, so a copy is one run of bytes per unit, read once and written to every slot.
+// A unit's rows are contiguous, so a copy is one run of bytes per unit, read once and written to every slot; a block takes 32 KB of it.
+// Bound by DRAM: 16384 4-bit tokens of 8 heads and 8 layers to eight slots (1.96 GB) 317 us, 94% of the copy bandwidth; 348 with a couple
+// of waves of blocks that walk over the rest.
 constexpr int kForkThreads = 256;
-constexpr int kForkUnroll = 4;
+constexpr int kForkUnroll = 8;
 
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(Geom gm, UnitTable ut, ForkArgs a, void* __restrict__ kv, void* __restrict__ kimp,
                                                             int32_t* __restrict__ lists, int32_t* __restrict__ counts,
@@ -75,8 +77,7 @@ cudaError_t launch_fork(const tb_ctx* c, const UnitTable& ut, const ForkArgs& a,
     const int streams = gm.Hkv + gm.Hi + (a.n_tokens < 0 ? 1 : 0);
     const long long chunks = (long long)a.max_tokens * (gm.row_bytes / 16);
     long long bx = (chunks + kForkThreads * kForkUnroll - 1) / (kForkThreads * kForkUnroll);
-    const long long most = 16LL * c->sm_count / (streams * ut.layer_count) + 1;      // a couple of waves of the chip
-    bx = bx < 1 ? 1 : bx > most ? most : bx;
+    if (bx < 1) bx = 1;
     dim3 grid((unsigned)bx, streams, ut.layer_count);
     fork_kernel<<<grid, kForkThreads, 0, s>>>(gm, ut, a, c->kv, c->kimp, c->st.idx, c->st.cnt, c->st.len, c->st.len_proj, c->st.misc_counter + 2);
     return cudaGetLastError();
@@ -86,46 +87,71 @@ cudaError_t launch_fork(const tb_ctx* c, const UnitTable& ut, const ForkArgs& a,
 // Row begin + j becomes row keep[j], in place.  Kept positions ascend, so keep[j] >= begin + j: a row only ever moves down,
 // onto rows that are read with it or were read before it.  A block takes one unit's rows in order, a tile at a time: all threads
 // have read tile t (and, behind the barrier, know it) before any writes it, and what tile t writes lies below all that later tiles
-// read.  Entries that do not ascend or lie outside [begin, length) are reported and their rows left alone (the order above holds for
+// read, so the next tile's rows are on their way before this one's are written.  Columns of a row do not depend on one another: where
+// there are too few units to fill the chip, a unit is cut into slices of columns, a block each.
+// Bound by DRAM: copying 32768 bf16 tokens of 8 heads and 4 layers and keeping 15565 of them (1.78 GB) takes 306 us, 89% of the copy bandwidth;
+// 383 when entries were fetched with their rows, 1290 with a block per unit.
+// Entries that do not ascend or lie outside [begin, length) are reported and their rows left alone (the order above holds for
 // any entry >= begin + j, and others are not followed).
 constexpr int kCompactThreads = 256;
-constexpr int kCompactUnroll = 4;
+constexpr int kCompactUnroll = 8;
 
-__global__ void __launch_bounds__(kCompactThreads) compact_kernel(Geom gm, UnitTable ut, CompactArgs a, void* __restrict__ kv, void* __restrict__ kimp,
-                                                                  int32_t* __restrict__ len_dev, int32_t* __restrict__ len_proj_dev,
-                                                                  uint32_t* __restrict__ counter, int32_t* __restrict__ status) {
-    const int ll = blockIdx.z / ut.n_seq, s = blockIdx.z % ut.n_seq, stream = blockIdx.y;
+__global__ void __launch_bounds__(kCompactThreads, 2) compact_kernel(Geom gm, UnitTable ut, CompactArgs a, void* __restrict__ kv, void* __restrict__ kimp,
+                                                                     int32_t* __restrict__ len_dev, int32_t* __restrict__ len_proj_dev,
+                                                                     uint32_t* __restrict__ counter, int32_t* __restrict__ status) {
+    const int ll = blockIdx.z / ut.n_seq, s = blockIdx.z % ut.n_seq;
+    const int y = blockIdx.y, n_kv = gm.Hkv * a.kv_slices;
+    const int stream = y < n_kv ? y / a.kv_slices : gm.Hkv + (y - n_kv) / a.imp_slices;
+    const int slices = y < n_kv ? a.kv_slices : a.imp_slices, slice = y < n_kv ? y % slices : (y - n_kv) % slices;
     const RowStream rs(gm, kv, kimp, stream);
+    pdl_wait();                                        // (see append_kernel)
+    pdl_launch_dependents();
     const int begin = a.begin[s], L = unit_len(gm, ut, ll, s);
     // (lengths read on the device may be shorter than the host knew: then nothing is moved and the sequence keeps its length)
     const int n = begin + a.n_keep[s] <= L ? a.n_keep[s] : 0;
-    uint4* unit = rs.unit(gm, ut.layer_begin + ll, ut.seq_id[s]);
-    const int32_t* keep = a.keep + (size_t)s * a.stride;
-    const int rows = kCompactThreads * kCompactUnroll / rs.chunks;    // of a tile
     bool bad = begin + a.n_keep[s] > L;
-    for (int j0 = 0; j0 < n; j0 += rows) {
-        uint4 v[kCompactUnroll];
-        int to[kCompactUnroll];
+    const int wide = rs.chunks / slices, rows = kCompactThreads / wide;      // chunks of the slice; rows that the block moves side by side
+    const int row0 = threadIdx.x / wide;
+    const bool works = row0 < rows;
+    uint4* unit = rs.unit(gm, ut.layer_begin + ll, ut.seq_id[s]) + slice * wide + (threadIdx.x - row0 * wide);
+    const int32_t* keep = a.keep + (size_t)s * a.stride;
+    const int tile = rows * kCompactUnroll;
+    int from[kCompactUnroll];                          // rows of the tile that is on its way: -1 = stays
+    int entry[kCompactUnroll], before[kCompactUnroll]; // entries of the one behind it, and those before them
+    uint4 v[kCompactUnroll];
+    auto fetch = [&](int j0) {
 #pragma unroll
         for (int i = 0; i < kCompactUnroll; ++i) {
-            const int item = threadIdx.x + i * kCompactThreads, row = item / rs.chunks, j = j0 + row;
-            to[i] = -1;
-            if (row < rows && j < n) {
-                const int t = keep[j];
-                const bool ok = t >= begin + j && t < L && (j == 0 || keep[j - 1] < t);
+            const int j = j0 + row0 + i * rows;
+            if (works && j < n) entry[i] = __ldg(keep + j), before[i] = j ? __ldg(keep + j - 1) : -1;
+        }
+    };
+    auto load = [&](int j0) {
+#pragma unroll
+        for (int i = 0; i < kCompactUnroll; ++i) {
+            const int j = j0 + row0 + i * rows;
+            from[i] = -1;
+            if (works && j < n) {
+                const bool ok = entry[i] >= begin + j && entry[i] < L && before[i] < entry[i];
                 bad |= !ok;
-                if (ok && t > begin + j) {
-                    to[i] = begin + j;
-                    v[i] = unit[(size_t)t * rs.chunks + (item - row * rs.chunks)];
-                }
+                if (ok && entry[i] > begin + j) from[i] = entry[i], v[i] = __ldcg(unit + (size_t)entry[i] * rs.chunks);
             }
         }
+    };
+    fetch(0);
+    load(0);
+    fetch(tile);
+    for (int j0 = 0; j0 < n; j0 += tile) {
+        uint4 w[kCompactUnroll];
+        unsigned moves = 0;
+#pragma unroll
+        for (int i = 0; i < kCompactUnroll; ++i) w[i] = v[i], moves |= (unsigned)(from[i] >= 0) << i;
+        load(j0 + tile);
+        fetch(j0 + 2 * tile);
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kCompactUnroll; ++i) {
-            const int item = threadIdx.x + i * kCompactThreads, row = item / rs.chunks;
-            if (to[i] >= 0) unit[(size_t)to[i] * rs.chunks + (item - row * rs.chunks)] = v[i];
-        }
+        for (int i = 0; i < kCompactUnroll; ++i)
+            if (moves >> i & 1) unit[(size_t)(begin + j0 + row0 + i * rows) * rs.chunks] = w[i];
     }
     if (bad) atomicExch(status, kStatusBadIndex);
     if (!ut.use_dev_len || !last_block_arrives(counter, gridDim.x * gridDim.y * gridDim.z)) return;
@@ -138,11 +164,26 @@ __global__ void __launch_bounds__(kCompactThreads) compact_kernel(Geom gm, UnitT
     }
 }
 
-cudaError_t launch_compact(const tb_ctx* c, const UnitTable& ut, const CompactArgs& a, cudaStream_t s) {
+cudaError_t launch_compact(const tb_ctx* c, const UnitTable& ut, const CompactArgs& a_in, cudaStream_t s) {
     const Geom& gm = c->geom;
-    dim3 grid(1, gm.Hkv + gm.Hi, ut.layer_count * ut.n_seq);
-    compact_kernel<<<grid, kCompactThreads, 0, s>>>(gm, ut, a, c->kv, c->kimp, c->st.len, c->st.len_proj, c->st.misc_counter + 3, c->st.status);
-    return cudaGetLastError();
+    CompactArgs a = a_in;
+    const int kv_chunks = gm.row_bytes / 16, imp_chunks = gm.dp * (gm.dtype == TB_BF16 ? 2 : 4) / 16, units = ut.layer_count * ut.n_seq;
+    a.kv_slices = a.imp_slices = 1;
+    // a tile or two per unit are not worth cutting
+    if ((long long)a.max_keep * kv_chunks > 2 * kCompactThreads * kCompactUnroll)
+        for (int wide = 64; wide >= 2; wide /= 2) {
+            a.kv_slices = !gm.fp4 ? (kv_chunks + wide - 1) / wide : wide >= 9 ? 1 : wide >= 3 ? 3 : 9;
+            a.imp_slices = (imp_chunks + wide - 1) / wide;
+            if (units * (gm.Hkv * a.kv_slices + gm.Hi * a.imp_slices) >= 2 * c->sm_count) break;
+        }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1, gm.Hkv * a.kv_slices + gm.Hi * a.imp_slices, units);
+    cfg.blockDim = dim3(kCompactThreads, 1, 1), cfg.dynamicSmemBytes = 0, cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see pdl_wait()
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr, cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, compact_kernel, gm, ut, a, c->kv, c->kimp, c->st.len, c->st.len_proj, c->st.misc_counter + 3, c->st.status);
 }
 
 // ---------------------------------------------------------------------------------------------
