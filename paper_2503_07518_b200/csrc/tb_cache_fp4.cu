@@ -261,7 +261,10 @@ __global__ void __launch_bounds__(kProjFp4Threads, kWalk ? 3 : 6) project_fp4_ke
     __shared__ __align__(16) unsigned char ring[kWalk ? kProjFp4Threads / 32 * kProjAhead * 16 * kProjRow : 16];
     const int ll = blockIdx.z / ut.n_seq, s = blockIdx.z % ut.n_seq, h = blockIdx.y;
     const int layer = ut.layer_begin + ll, warp = threadIdx.x >> 5;
-    pdl_wait();                                        // (rows, and lengths read on the device, may come from the predecessor)
+    // The (first) matrix is fetched beside the predecessor's tail: tb_set_projection's copy is no kernel, so it was complete when the predecessor
+    // began.  Rows, and lengths read on the device, may be the predecessor's.
+    stage_projection<DP>(Wall + ((size_t)layer * gm.Hkv + (kWalk ? h : h * (gm.Hkv / gm.Hi))) * D * DP, Ws);
+    pdl_wait();
     pdl_launch_dependents();
     int begin, end;
     project_range(gm, ut, pt, ll, s, begin, end);
@@ -282,7 +285,6 @@ __global__ void __launch_bounds__(kProjFp4Threads, kWalk ? 3 : 6) project_fp4_ke
                 if ((long long)first + (long long)i * step < end) KeyTile::ask(stages_u32 + i * 16 * kProjRow, rows, first + i * step, end);
                 asm volatile("cp.async.commit_group;" ::: "memory");
             }
-            stage_projection<DP>(Wall + ((size_t)layer * gm.Hkv + h) * D * DP, Ws);
             __syncthreads();
             uint32_t b[8][NT / 2][4];
 #pragma unroll
@@ -348,6 +350,7 @@ __global__ void __launch_bounds__(kProjFp4Threads, kWalk ? 3 : 6) project_fp4_ke
     } else {
         // (one key stream per layer: the heads' projections are summed in the accumulators, heads in ascending order)
         const int n_sum = gm.Hkv / gm.Hi;
+        int staged = h * n_sum;                        // whose matrix is in shared memory
         constexpr int kTiles = 2, kTokens = kProjFp4Threads / 32 * 16 * kTiles;
         for (int t0 = begin + blockIdx.x * kTokens; t0 < end; t0 += gridDim.x * kTokens) {
             const int tw = t0 + warp * 16 * kTiles;
@@ -361,9 +364,12 @@ __global__ void __launch_bounds__(kProjFp4Threads, kWalk ? 3 : 6) project_fp4_ke
                 KeyTile tile[kTiles];
 #pragma unroll
                 for (int i = 0; i < kTiles; ++i) tile[i].load(rows, min(tw + 16 * i, end - 1), end);
-                __syncthreads();                                       // the previous matrix has been read
-                stage_projection<DP>(Wall + ((size_t)layer * gm.Hkv + hk) * D * DP, Ws);
-                __syncthreads();
+                __syncthreads();                                       // the previous matrix has been read, or the first one written
+                if (hk != staged) {
+                    stage_projection<DP>(Wall + ((size_t)layer * gm.Hkv + hk) * D * DP, Ws);
+                    staged = hk;
+                    __syncthreads();
+                }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     uint32_t a[kTiles][2][4];

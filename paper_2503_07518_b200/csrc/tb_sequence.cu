@@ -88,7 +88,8 @@ cudaError_t launch_fork(const tb_ctx* c, const UnitTable& ut, const ForkArgs& a,
 // onto rows that are read with it or were read before it.  A block takes one unit's rows in order, a tile at a time: all threads
 // have read tile t (and, behind the barrier, know it) before any writes it, and what tile t writes lies below all that later tiles
 // read, so the next tile's rows are on their way before this one's are written.  Columns of a row do not depend on one another: where
-// there are too few units to fill the chip, a unit is cut into slices of columns, a block each.
+// there are too few units to fill the chip, a unit is cut into slices of columns, a block each.  A few rows per unit (accepted drafts) are a
+// warp's work instead (kGroup threads; 1024 units of 8 rows: %WARP%).
 // Bound by DRAM: copying 32768 bf16 tokens of 8 heads and 4 layers and keeping 15565 of them (1.78 GB) takes 306 us, 89% of the copy bandwidth;
 // 383 when entries were fetched with their rows, 1290 with a block per unit.
 // Entries that do not ascend or lie outside [begin, length) are reported and their rows left alone (the order above holds for
@@ -96,11 +97,15 @@ cudaError_t launch_fork(const tb_ctx* c, const UnitTable& ut, const ForkArgs& a,
 constexpr int kCompactThreads = 256;
 constexpr int kCompactUnroll = 8;
 
+template <int kGroup>
 __global__ void __launch_bounds__(kCompactThreads, 2) compact_kernel(Geom gm, UnitTable ut, CompactArgs a, void* __restrict__ kv, void* __restrict__ kimp,
                                                                      int32_t* __restrict__ len_dev, int32_t* __restrict__ len_proj_dev,
                                                                      uint32_t* __restrict__ counter, int32_t* __restrict__ status) {
-    const int ll = blockIdx.z / ut.n_seq, s = blockIdx.z % ut.n_seq;
-    const int y = blockIdx.y, n_kv = gm.Hkv * a.kv_slices;
+    const int n_kv = gm.Hkv * a.kv_slices, n_streams = n_kv + gm.Hi * a.imp_slices;
+    const int group = blockIdx.x * (kCompactThreads / kGroup) + threadIdx.x / kGroup, me = threadIdx.x % kGroup;
+    const bool there = group < n_streams * ut.layer_count * ut.n_seq;  // (the last block's groups may be more than are left)
+    const int z = there ? group / n_streams : 0, y = there ? group % n_streams : 0;
+    const int ll = z / ut.n_seq, s = z % ut.n_seq;
     const int stream = y < n_kv ? y / a.kv_slices : gm.Hkv + (y - n_kv) / a.imp_slices;
     const int slices = y < n_kv ? a.kv_slices : a.imp_slices, slice = y < n_kv ? y % slices : (y - n_kv) % slices;
     const RowStream rs(gm, kv, kimp, stream);
@@ -108,12 +113,12 @@ __global__ void __launch_bounds__(kCompactThreads, 2) compact_kernel(Geom gm, Un
     pdl_launch_dependents();
     const int begin = a.begin[s], L = unit_len(gm, ut, ll, s);
     // (lengths read on the device may be shorter than the host knew: then nothing is moved and the sequence keeps its length)
-    const int n = begin + a.n_keep[s] <= L ? a.n_keep[s] : 0;
+    const int n = there && begin + a.n_keep[s] <= L ? a.n_keep[s] : 0;
     bool bad = begin + a.n_keep[s] > L;
-    const int wide = rs.chunks / slices, rows = kCompactThreads / wide;      // chunks of the slice; rows that the block moves side by side
-    const int row0 = threadIdx.x / wide;
+    const int wide = rs.chunks / slices, rows = kGroup / wide;        // chunks of the slice; rows that the group moves side by side
+    const int row0 = me / wide;
     const bool works = row0 < rows;
-    uint4* unit = rs.unit(gm, ut.layer_begin + ll, ut.seq_id[s]) + slice * wide + (threadIdx.x - row0 * wide);
+    uint4* unit = rs.unit(gm, ut.layer_begin + ll, ut.seq_id[s]) + slice * wide + (me - row0 * wide);
     const int32_t* keep = a.keep + (size_t)s * a.stride;
     const int tile = rows * kCompactUnroll;
     int from[kCompactUnroll];                          // rows of the tile that is on its way: -1 = stays
@@ -148,7 +153,8 @@ __global__ void __launch_bounds__(kCompactThreads, 2) compact_kernel(Geom gm, Un
         for (int i = 0; i < kCompactUnroll; ++i) w[i] = v[i], moves |= (unsigned)(from[i] >= 0) << i;
         load(j0 + tile);
         fetch(j0 + 2 * tile);
-        __syncthreads();
+        if constexpr (kGroup == 32) __syncwarp();
+        else __syncthreads();
 #pragma unroll
         for (int i = 0; i < kCompactUnroll; ++i)
             if (moves >> i & 1) unit[(size_t)(begin + j0 + row0 + i * rows) * rs.chunks] = w[i];
@@ -169,21 +175,30 @@ cudaError_t launch_compact(const tb_ctx* c, const UnitTable& ut, const CompactAr
     CompactArgs a = a_in;
     const int kv_chunks = gm.row_bytes / 16, imp_chunks = gm.dp * (gm.dtype == TB_BF16 ? 2 : 4) / 16, units = ut.layer_count * ut.n_seq;
     a.kv_slices = a.imp_slices = 1;
-    // a tile or two per unit are not worth cutting
-    if ((long long)a.max_keep * kv_chunks > 2 * kCompactThreads * kCompactUnroll)
+    // up to two of a warp's tiles: a warp each, its rows at most 32 chunks wide; up to two of a block's are not worth cutting
+    const long long kv_work = (long long)a.max_keep * kv_chunks;
+    const bool warps = kv_work <= 2 * 32 * kCompactUnroll;
+    if (warps) {
+        a.kv_slices = (kv_chunks + 31) / 32;
+    } else if (kv_work > 2 * kCompactThreads * kCompactUnroll) {
         for (int wide = 64; wide >= 2; wide /= 2) {
             a.kv_slices = !gm.fp4 ? (kv_chunks + wide - 1) / wide : wide >= 9 ? 1 : wide >= 3 ? 3 : 9;
             a.imp_slices = (imp_chunks + wide - 1) / wide;
             if (units * (gm.Hkv * a.kv_slices + gm.Hi * a.imp_slices) >= 2 * c->sm_count) break;
         }
+    }
+    const int groups = units * (gm.Hkv * a.kv_slices + gm.Hi * a.imp_slices), per_block = warps ? kCompactThreads / 32 : 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(1, gm.Hkv * a.kv_slices + gm.Hi * a.imp_slices, units);
+    cfg.gridDim = dim3((groups + per_block - 1) / per_block, 1, 1);
     cfg.blockDim = dim3(kCompactThreads, 1, 1), cfg.dynamicSmemBytes = 0, cfg.stream = s;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see pdl_wait()
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr, cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, compact_kernel, gm, ut, a, c->kv, c->kimp, c->st.len, c->st.len_proj, c->st.misc_counter + 3, c->st.status);
+    auto launch = [&](auto kernel) {
+        return cudaLaunchKernelEx(&cfg, kernel, gm, ut, a, c->kv, c->kimp, c->st.len, c->st.len_proj, c->st.misc_counter + 3, c->st.status);
+    };
+    return warps ? launch(compact_kernel<32>) : launch(compact_kernel<kCompactThreads>);
 }
 
 // ---------------------------------------------------------------------------------------------
