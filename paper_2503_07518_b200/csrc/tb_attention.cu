@@ -422,7 +422,7 @@ __device__ __forceinline__ void fp4_rows(const __nv_bfloat16* __restrict__ qbase
         uint32_t top2 = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint4 v = head < g ? __ldg(reinterpret_cast<const uint4*>(qbase + head * D + tig * 32) + i) : make_uint4(0u, 0u, 0u, 0u);
+            const uint4 v = head < g ? __ldcg(reinterpret_cast<const uint4*>(qbase + head * D + tig * 32) + i) : make_uint4(0u, 0u, 0u, 0u);
             w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
         }
 #pragma unroll
@@ -437,7 +437,9 @@ __device__ __forceinline__ void fp4_rows(const __nv_bfloat16* __restrict__ qbase
             qb[ks][0] = pack_f16(bf16_lo(w[2 * ks]) * up, bf16_hi(w[2 * ks]) * up);
             qb[ks][1] = pack_f16(bf16_lo(w[2 * ks + 1]) * up, bf16_hi(w[2 * ks + 1]) * up);
         }
-        xs[0] = qscale * __shfl_sync(0xffffffffu, down, tig * 8), xs[1] = qscale * __shfl_sync(0xffffffffu, down, tig * 8 + 4);
+        // (never zero, so that a masked score stays minus infinity: a query of zeros under a very small scale)
+        xs[0] = fmaxf(qscale * __shfl_sync(0xffffffffu, down, tig * 8), 1.1754944e-38f);
+        xs[1] = fmaxf(qscale * __shfl_sync(0xffffffffu, down, tig * 8 + 4), 1.1754944e-38f);
     }
     float o[8][4];
 #pragma unroll

@@ -138,7 +138,7 @@ cudaError_t launch_read_fp4(const tb_ctx* c, const UnitTable& ut, const ReadTabl
 // consecutive outputs of its two tokens.
 // Codes become f16 pairs and are scaled there, exactly.  W_K is bf16; a warp that walks brings its matrix to f16 too, by a power of two that puts
 // the largest element in [2^13, 2^14): exact for elements down to 2^-31 of it.  Where one is smaller, and for few tokens, the keys are turned
-// into bf16 instead, also exactly, which costs three instructions per pair (1M rows x d' 32: 53 us like that, %PROJ_US% on f16).  The products and the
+// into bf16 instead, also exactly, which costs three instructions per pair (1M rows x d' 32: 53 us like that, 43 on f16).  The products and the
 // order of their sums are the same, and so are the results; one rounding, at the end.
 // kWalk: a block keeps the matrix in registers and walks over the tokens, each warp a tile of 16 at a time with the next kProjAhead on their
 // way.  Otherwise (few tokens per unit, or one key stream per layer, which sums the heads' projections) it is read from shared memory,

@@ -89,7 +89,7 @@ cudaError_t launch_fork(const tb_ctx* c, const UnitTable& ut, const ForkArgs& a,
 // have read tile t (and, behind the barrier, know it) before any writes it, and what tile t writes lies below all that later tiles
 // read, so the next tile's rows are on their way before this one's are written.  Columns of a row do not depend on one another: where
 // there are too few units to fill the chip, a unit is cut into slices of columns, a block each.  A few rows per unit (accepted drafts) are a
-// warp's work instead (kGroup threads; 1024 units of 8 rows: %WARP%).
+// warp's work instead (kGroup threads; 1024 units of 8 rows: 3.5 us behind the launch before, 6 with a block each).
 // Bound by DRAM: copying 32768 bf16 tokens of 8 heads and 4 layers and keeping 15565 of them (1.78 GB) takes 306 us, 89% of the copy bandwidth;
 // 383 when entries were fetched with their rows, 1290 with a block per unit.
 // Entries that do not ascend or lie outside [begin, length) are reported and their rows left alone (the order above holds for
@@ -128,7 +128,8 @@ __global__ void __launch_bounds__(kCompactThreads, 2) compact_kernel(Geom gm, Un
 #pragma unroll
         for (int i = 0; i < kCompactUnroll; ++i) {
             const int j = j0 + row0 + i * rows;
-            if (works && j < n) entry[i] = __ldg(keep + j), before[i] = j ? __ldg(keep + j - 1) : -1;
+            // (not through the read-only path: the predecessor may have written them while this kernel was already there)
+            if (works && j < n) entry[i] = __ldcg(keep + j), before[i] = j ? __ldcg(keep + j - 1) : -1;
         }
     };
     auto load = [&](int j0) {

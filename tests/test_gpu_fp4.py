@@ -249,6 +249,55 @@ def test_a_row_projects_alike_in_every_call(tb):
         assert torch.equal(ctx.kimp, whole)
 
 
+@pytest.mark.parametrize("n", [60, 700])
+@pytest.mark.parametrize("kind", ["wide", "tiny", "huge", "zero", "inf"])
+def test_projection_matrices_of_every_range(tb, n, kind):
+    """Elements 2^-40 below the largest (more than f16 spans), matrices of the smallest and largest magnitudes, of zeros, and with an infinity."""
+    g = generator(40)
+    ctx = context(tb, 1, 2, 2, 1, room=n)
+    W = torch.randn(1, 2, 128, 32, generator=g, device="cuda")
+    if kind == "wide":
+        W *= torch.exp2(torch.randint(-40, 1, W.shape, generator=g, device="cuda").float())
+    W = (W * {"tiny": 2.0 ** -110, "huge": 2.0 ** 90, "zero": 0.0}.get(kind, 1.0)).bfloat16()
+    if kind == "inf":
+        W[0, 1, 5, 7] = math.inf
+    ctx.W = W
+    ctx.set_projection(0, W[0])
+    k, v = rows(g, 1, n, 2, spread=1.0), rows(g, 1, n, 2)
+    k[:, :, :, ::3] = 0                                                    # (large elements of W against zeros: small ones count)
+    ctx.append_kv(0, 1, None, [n], k, v)
+    ctx.project_keys(0, 1, None, [0], [n])
+    if kind == "inf":
+        at = held(k)[0, :, 1, 5]
+        assert torch.equal(torch.isinf(ctx.kimp[0, 0, 1, :, 7]), at != 0) and torch.isnan(ctx.kimp[0, 0, 1, :, 7][at == 0]).all()
+        ctx.kimp[0, 0, 1, :, 7] = 0
+        ctx.W = torch.where(torch.isinf(W), torch.zeros_like(W), W)
+        ctx.W[0, 1, :, 7] = 0
+    check_projected(ctx, held(k)[0].transpose(0, 1), 0, n, 0, 0)
+
+
+def test_scores_and_selections_are_those_of_bf16(tb):
+    """The same projected keys: the same scores and lists, bit for bit."""
+    g = generator(41)
+    got = []
+    kimp = torch.randn(2, 3, 4, 900, 32, generator=g, device="cuda").bfloat16()
+    qi = torch.randn(2, 3, 8, 32, generator=g, device="cuda")
+    k = torch.zeros(2, 2700, 4, 128, dtype=torch.bfloat16, device="cuda")
+    for dt in (tb.TB_FP4, tb.TB_BF16):
+        ctx = tb.Context(2, 8, 4, 128, 32, dt, 3, 900, 100, 1)
+        ctx.append_kv(0, 2, None, [900] * 3, k, k)
+        ctx.project_keys(0, 2, None, [0] * 3, [900] * 3)
+        ctx.kimp.copy_(kimp)
+        idx = torch.zeros(2, 3, 4, ctx.index_capacity, dtype=torch.int32, device="cuda")
+        cnt = torch.zeros(2, 3, 4, dtype=torch.int32, device="cuda")
+        ctx.select_topk(0, 2, None, 3, qi, tb.select_params(100, 4, 16, 1), idx, cnt)
+        scores = torch.zeros(3, 4, 900, device="cuda")
+        ctx.score_tokens(1, None, 3, qi[1].contiguous(), scores)
+        assert ctx.get_status() == 0
+        got.append((idx, cnt, scores))
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and (got[0][1] > 100).all()
+
+
 # ---- attention ----------------------------------------------------------------------------------------------------------
 
 def reference(q, k, v, seen, scale):
@@ -362,6 +411,20 @@ def test_large_and_small_queries_and_values(tb):
     q[0, 0, 7, :64] *= 2.0 ** -20
     check_attention(tb, ctx, held(k), held(v), [200], tb.select_params(-1), q)
     check_attention(tb, ctx, held(k), held(v), [200], tb.select_params(-1), q, scale=0.7)
+
+
+def test_masked_scores_of_a_query_of_zeros(tb):
+    """Lists shorter than a tile, a query of zeros and scales down to nearly nothing: the rows that are there share the weight."""
+    g = generator(42)
+    ctx = context(tb, 1, 4, 1, 1, room=64, budget=8)
+    k, v = rows(g, 1, 50, 1), rows(g, 1, 50, 1)
+    ctx.append_kv(0, 1, None, [50], k, v)
+    idx = torch.tensor([[[[7, 9, 30, 41, 0, 0, 0, 0]]]], dtype=torch.int32, device="cuda")
+    cnt = torch.tensor([[[4]]], dtype=torch.int32, device="cuda")
+    q = torch.zeros(1, 1, 4, 128, dtype=torch.bfloat16, device="cuda")
+    for scale in (0.0, 1e-12, 1e-30):
+        out, _ = check_attention(tb, ctx, held(k), held(v), [50], tb.select_params(8), q, idx, cnt, scale=scale)
+        assert (out[0, 0].double() - held(v)[0, [7, 9, 30, 41], 0].mean(0)).abs().max() <= 1e-6
 
 
 def test_many_small_weights_beside_one_large(tb):
