@@ -243,6 +243,9 @@ def prepare(case, seed):
             s.ctx.append_kv(0, layers, None, i.new, i.k_new, i.v_new)
         if c["kind"] == "attend":
             s.params = tb.select_params(c["budget"], c["sinks"], c["recent"])
+            s.results = {"out": torch.empty(layers, B, c["q_heads"], HEAD_DIM, device="cuda"), "lse": torch.empty(layers, B, c["q_heads"], device="cuda")}
+            lists = zip(i.idx, i.cnt) if c["budget"] >= 0 else [(None, None)] * layers
+            s.by_layer = [(*t, *u) for t, u in zip(zip(i.q, s.results["out"], s.results["lse"]), lists)]      # a layer's tensors are its own in a decode step
         s.seen = _seen(s)
     else:
         s.kv = torch.zeros(layers, slots, heads, room, ROW, dtype=torch.uint8, device="cuda") if fp4 else \
@@ -274,11 +277,9 @@ def run(state):
 def _run_own(s):
     c, kind, B = s.c, s.c["kind"], len(s.cached)
     if kind == "attend":
-        lists = c["budget"] >= 0
-        for l in range(c["layers"]):
-            s.ctx.sparse_decode_attention(l, 1, None, B, s.q[l], s.params, s.out[l], idx=s.idx[l] if lists else None,
-                                          cnt=s.cnt[l] if lists else None, lse=s.lse[l])
-        return {"out": s.out, "lse": s.lse}
+        for l, (q, out, lse, idx, cnt) in enumerate(s.by_layer):
+            s.ctx.sparse_decode_attention(l, 1, None, B, q, s.params, out, idx=idx, cnt=cnt, lse=lse)
+        return s.results
     if kind == "ingest":
         s.ctx.compact_sequences(None, s.cached)                          # rolls the rows of the last pass back
         s.ctx.append_kv(0, c["layers"], None, s.new, s.k_new, s.v_new)
