@@ -386,6 +386,10 @@ __device__ __forceinline__ void f32_rows(const float* __restrict__ qbase, int g,
 // The tensor core truncates as it accumulates, about 2e-8 of the sum per mma, which adds up over the tiles of a long sequence (3.8e-6 of the
 // result at 120,000 tokens).  So O moves into fp32 sums in shared memory every kFp4Flush tiles; adding every pair of tiles in registers took
 // 32 of its 630 instructions.
+// What bounds it: the conversions, their scaling (64 lanes per clock each) and the mma together take 4.3 clocks of an SM per row, the rest two more,
+// and a row's 144 bytes six at the copy bandwidth: 16 problems of 110,000 rows 59.5 us, 65% of it; the bf16 rows of the same tokens 131.
+// Gathered rows cost 192 bytes of DRAM each (three accesses of 64), and a launch of them a chain of lists, rows, two or three tiles per warp
+// and a merge.
 // Leaves accumulators and statistics parked as the bf16 warp does, but for the channels: float4 number mt * 32 + lane holds
 // channels 16 gid + 2 mt and + 1 (kNarrow: of heads 2 tig and + 1 in lanes tig < 2, their low parts in lanes tig + 2).
 constexpr int kFp4Tile = 32;                          // rows of a stage

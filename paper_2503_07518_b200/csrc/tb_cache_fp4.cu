@@ -8,8 +8,9 @@
 namespace tb {
 
 // A thread quantises one block of 16 channels: 32 bytes in, 8 bytes of codes and a scale byte out; 16 neighbours share a
-// (token, head).  A block belongs to one (layer, sequence).  Bound by DRAM bandwidth for prompts (512 bytes read, 144 written per
-// token and head) and by the launch for a decode token.
+// (token, head).  A block belongs to one (layer, sequence).  512 bytes read and 144 written per token and head: 424,000 of them in 52 us, 5.4 TB/s
+// (82% of the copy bandwidth), the conversions taking 63% of the ALU's cycles; bound by the launch for a decode token.  With one 32-byte access
+// per thread instead of two of 16 and no division; before, 64 us; two blocks of channels in flight per thread instead of four, 7% slower.
 constexpr int kQuantThreads = 256;
 constexpr int kQuantUnroll = 4;
 constexpr int kQuantPairs = kQuantThreads / 16 * kQuantUnroll;        // (token, head) pairs of a block
@@ -85,7 +86,8 @@ cudaError_t launch_append_fp4(const tb_ctx* c, const UnitTable& ut, const int* n
 }
 
 // ---------------------------------------------------------------------------------------------
-// Rows as values: a thread turns 8 bytes of codes and a scale into 16 bf16 channels (exact), kReadUnroll of them in flight.
+// Rows as values: a thread turns 8 bytes of codes and a scale into 16 bf16 channels (exact), kReadUnroll of them in flight.  Bound by
+// DRAM: 144 bytes in, 512 out, 424,000 rows in 43 us (6.4 TB/s).
 constexpr int kReadUnroll = 4;
 constexpr int kReadPairs = kQuantThreads / 16 * kReadUnroll;
 
@@ -143,7 +145,8 @@ cudaError_t launch_read_fp4(const tb_ctx* c, const UnitTable& ut, const ReadTabl
 // kWalk: a block keeps the matrix in registers and walks over the tokens, each warp a tile of 16 at a time with the next kProjAhead on their
 // way.  Otherwise (few tokens per unit, or one key stream per layer, which sums the heads' projections) it is read from shared memory,
 // two tiles at a time, and twice as many blocks are resident.
-// Bound by DRAM: 96 of a row's 144 bytes (three sectors) in, 2 d' out.
+// Bound by DRAM: of a row's 144 bytes 96 are asked for (three sectors), but memory is read 64 bytes at a time and that is all of it, so 144 in and
+// 2 d' out: 1M rows, d' 32, 218 MB in 41 us (5.3 TB/s); rows prefetched into registers 46, 64 tokens and a matrix per block 99.
 constexpr int kProjFp4Threads = 128;
 constexpr int kProjAhead = 6;
 constexpr int kProjRow = 80;                           // bytes of a row that a tile needs: K codes and both halves' scales
