@@ -171,6 +171,15 @@ PyObject* append_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call([&] { return tb_append_kv((tb_ctx*)ctx, lb, lc, ids.data, n_new.data, (int32_t)n_new.n, k, v, stream); });
 }
 
+// What a kernel reads or writes as one run of bytes: a torch tensor has to be one, on a device, and of the type that is asked for.
+bool is_dense(PyObject* o, bool ints, const char* what) {
+    if (!THPVariable_Check(o)) return true;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.is_cuda() && t.is_contiguous() && (!ints || t.scalar_type() == at::kInt)) return true;
+    PyErr_Format(PyExc_ValueError, "%s: a contiguous %sCUDA tensor is expected", what, ints ? "int32 " : "");
+    return false;
+}
+
 // (ctx, layer_begin, layer_count, seq_ids, pos_begin, pos_end, k_out, v_out, stream)
 PyObject* read_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void *ctx, *k, *v, *stream;
@@ -179,7 +188,7 @@ PyObject* read_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!want(n, 9) || !read_address(a[0], &ctx) || !read_int(a[1], &lb) || !read_int(a[2], &lc) || !ids.read(a[3]) || !pb.read(a[4]) ||
         !pe.read(a[5]) || !read_pointer(a[6], &k) || !read_pointer(a[7], &v) || !read_stream(a[8], &stream))
         return nullptr;
-    if (!same_length(ids, pb) || !same_length(pe, pb)) return nullptr;
+    if (!same_length(ids, pb) || !same_length(pe, pb) || !is_dense(a[6], false, "k_out") || !is_dense(a[7], false, "v_out")) return nullptr;
     return call([&] { return tb_read_kv((tb_ctx*)ctx, lb, lc, ids.data, pb.data, pe.data, (int32_t)pb.n, k, v, stream); });
 }
 
@@ -202,7 +211,7 @@ PyObject* compact_sequences(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!want(n, 6) || !read_address(a[0], &ctx) || !ids.read(a[1]) || !begin.read(a[2]) || !keep.read(a[3]) ||
         (a[4] != Py_None && !read_matrix(a[4], &idx, &rows, &stride)) || !read_stream(a[5], &stream))
         return nullptr;
-    if (!same_length(ids, begin) || !same_length(keep, begin)) return nullptr;
+    if (!same_length(ids, begin) || !same_length(keep, begin) || !is_dense(a[4], true, "keep_idx")) return nullptr;
     if (idx && rows < (int32_t)begin.n) {
         PyErr_SetString(PyExc_ValueError, "a row of positions per sequence is expected");
         return nullptr;

@@ -55,6 +55,18 @@ def test_the_extension_module_checks_the_lengths_of_its_lists(b):
         b._calls.fork_sequence(None, 0, None)
 
 
+def test_tensors_that_a_kernel_could_not_read_are_refused(b):
+    """On the host, of another type, or not one run of bytes (the type and the strides are asked for on the device too)."""
+    import torch
+    s = type("Stream", (), {"cuda_stream": 0})()
+    for idx in (torch.zeros(1, 4, dtype=torch.int32), torch.zeros(1, 4, dtype=torch.int64)):
+        with pytest.raises(ValueError, match="keep_idx"):
+            b._calls.compact_sequences(None, None, [0], [1], idx, s)
+    for k, v in ((torch.zeros(4), None), (None, torch.zeros(4))):
+        with pytest.raises(ValueError, match="_out"):
+            b._calls.read_kv(None, 0, 1, None, [0], [1], k, v, s)
+
+
 def test_types_that_a_4_bit_context_takes(b):
     import torch
     assert b.torch_dtype(b.TB_FP4) == b.torch_dtype(b.TB_BF16) == torch.bfloat16 and b.torch_dtype(b.TB_F32) == torch.float32

@@ -185,6 +185,21 @@ def test_ragged_appends_and_reads(tb, hkv, layers, counts):
         off += m
 
 
+def test_rows_that_start_on_16_bytes(tb):
+    """Inputs and outputs aligned to 16 bytes but not to 32: the same rows."""
+    g = generator(43)
+    ctx = context(tb, 2, 8, 2, 2, room=200)
+    room = torch.zeros(2, 2 * 90 * 2 * 128 + 8, dtype=torch.bfloat16, device="cuda")
+    k, v = (room[i, 8:].view(2, 90, 2, 128) for i in range(2))
+    room = torch.zeros(2, 2 * 90 * 2 * 128 + 8, dtype=torch.bfloat16, device="cuda")
+    ko, vo = (room[i, 8:].view(2, 90, 2, 128) for i in range(2))
+    assert k.data_ptr() % 32 == 16 and ko.data_ptr() % 32 == 16
+    k.copy_(rows(g, 2, 90, 2)), v.copy_(rows(g, 2, 90, 2))
+    ctx.append_kv(0, 2, None, [40, 50], k, v)
+    ctx.read_kv(0, 2, None, [0, 0], [40, 50], ko, vo)
+    assert torch.equal(ko.double(), held(k)) and torch.equal(vo.double(), held(v)) and (room[:, :8] == 0).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_reads_of_the_other_types_return_what_was_appended(tb, dtype):
     dt = tb.TB_BF16 if dtype == "bf16" else tb.TB_F32
@@ -649,4 +664,7 @@ def test_refusals(tb):
     for bad in ([0], [0, 0], [0, 0, 0, 0]):
         with pytest.raises(ValueError):
             ctx.read_kv(0, 2, None, bad, [4, 4, 4], k, k)
+    for bad in (k.transpose(0, 1), k.cpu(), k[:, ::2]):
+        with pytest.raises(ValueError):
+            ctx.read_kv(0, 2, None, [0] * 3, [10] * 3, bad, k)
     assert ctx.get_status() == 0

@@ -278,6 +278,10 @@ def test_compaction_refusals(tb):
         with pytest.raises(tb.TBError) as e:
             ctx.compact_sequences(*a)
         assert e.value.status == status and ctx.launch_count() == n0, a
+    wide = torch.zeros(2, 16, dtype=torch.int32, device="cuda")
+    for bad in (wide[:, ::2], wide.long(), wide.cpu(), wide.t()):
+        with pytest.raises(ValueError):
+            ctx.compact_sequences([0], [0], [1], bad)
     for a in (([0], [0, 0], [1, 1], idx), ([0, 1], [0, 0], [1], idx), ([0, 1, 2], [0, 0, 0], [1, 1, 0], idx)):
         with pytest.raises(ValueError):
             ctx.compact_sequences(*a)
@@ -380,6 +384,44 @@ def test_speculative_decoding_of_two_samples(tb, name, host, resident, devlen):
         ctx.sync_lengths()
         assert lengths(ctx, 1)[0] == n[1] and lengths(ctx, 2)[0] == n[2]
     assert ctx.get_status() == 0 and plain.get_status() == 0
+
+
+@pytest.mark.parametrize("name", TYPES)
+def test_drafts_verified_in_a_replayed_graph(tb, name):
+    """Truncate, append, project, compact and attend captured once: every replay verifies the new drafts at the same place."""
+    ctx = make(tb, name, hq=8, batch=2, room=300)
+    grow(ctx, 0, 150)
+    k, v = (torch.zeros(2, 9, 2, 128, dtype=ctx.dt, device="cuda") for _ in range(2))
+    idx, q, out = torch.zeros(1, 4, dtype=torch.int32, device="cuda"), torch.zeros(2, 1, 8, 128, dtype=ctx.dt, device="cuda"), torch.zeros(2, 1, 8, 128, device="cuda")
+
+    def step():
+        ctx.compact_sequences([0], [150])
+        ctx.append_kv(0, 2, [0], [9], k, v)
+        ctx.project_keys(0, 2, [0], [150], [159])
+        ctx.compact_sequences([0], [150], [4], idx)
+        ctx.sparse_decode_attention(0, 2, [0], 1, q, tb.select_params(-1), out)
+
+    idx.copy_(torch.tensor([[150, 151, 152, 153]], dtype=torch.int32))
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in range(3):
+        for t in (k, v, q):
+            t.copy_(torch.randn(t.shape, generator=ctx.g, device="cuda"))
+        at = torch.tensor([0, 2 + seed, 6, 8 - (seed == 2)])
+        idx.copy_((150 + at)[None].to(torch.int32))
+        graph.replay()
+        direct = make(tb, name, hq=8, batch=2, room=300)
+        grow(direct, 0, 150)
+        direct.append_kv(0, 2, [0], [4], k[:, at].contiguous(), v[:, at].contiguous())
+        direct.project_keys(0, 2, [0], [150], [154])
+        want = torch.zeros_like(out)
+        direct.sparse_decode_attention(0, 2, [0], 1, q, tb.select_params(-1), want)
+        assert torch.equal(ctx.kv[:, 0, :, :154], direct.kv[:, 0, :, :154]) and torch.equal(ctx.kimp[:, 0, :, :154], direct.kimp[:, 0, :, :154])
+        assert torch.equal(out, want) and torch.isfinite(out).all()
+    assert ctx.get_status() == 0 and lengths(ctx, 0) == (154, 154)
 
 
 def test_on_another_stream(tb):
