@@ -90,7 +90,7 @@ cudaError_t launch_fork(const tb_ctx* c, const UnitTable& ut, const ForkArgs& a,
 // read, so the next tile's rows are on their way before this one's are written.  Columns of a row do not depend on one another: where
 // there are too few units to fill the chip, a unit is cut into slices of columns, a block each.  A few rows per unit (accepted drafts) are a
 // warp's work instead (kGroup threads; 1024 units of 8 rows: 3.5 us behind the launch before, 6 with a block each).
-// Bound by DRAM: copying 32768 bf16 tokens of 8 heads and 4 layers and keeping 15565 of them (1.78 GB) takes 306 us, 89% of the copy bandwidth;
+// Bound by DRAM: copying 32768 bf16 tokens of 8 heads and 4 layers and keeping 15565 of them (1.78 GB) takes 300 us, 91% of the copy bandwidth;
 // 383 when entries were fetched with their rows, 1290 with a block per unit.
 // Entries that do not ascend or lie outside [begin, length) are reported and their rows left alone (the order above holds for
 // any entry >= begin + j, and others are not followed).
