@@ -181,8 +181,8 @@ tb_status tb_fork_sequence(tb_ctx* ctx, int32_t src_seq, const int32_t* dst_seqs
  * runs).  Rows and projected keys move, bit for bit; rows behind the new length are left as they are.  A layer's stored
  * selection stays if it was made while the layer held at most keep_begin[i] tokens (without device lengths), else it is dropped.  Bound resident rows are brought up to date.
  * An entry that does not ascend or lies outside the range sets TB_ERR_BAD_INDEX in the status word; its row holds what it held before.
- * With device lengths the counts are still those given here: a sequence that is shorter than they say keeps its rows and length, and is reported as
- * TB_ERR_BAD_INDEX.
+ * With device lengths the counts are still those given here.  A layer of a sequence that is shorter than they say keeps its rows and length, and is reported as
+ * TB_ERR_BAD_INDEX; so does one that is to keep tokens behind keep_begin of which some are projected and some not, reported as TB_ERR_UNPROJECTED.
  * TB_ERR_INVALID_ARG: keep_begin + n_keep beyond a layer's length, n_keep beyond keep_stride; TB_ERR_UNPROJECTED: tokens are
  * kept behind keep_begin of which some are projected and some not. */
 tb_status tb_compact_sequences(tb_ctx* ctx, const int32_t* seq_ids, int32_t n_seq, const int32_t* keep_begin, const int32_t* n_keep,
@@ -310,8 +310,8 @@ typedef struct {
 tb_status tb_predict_importance_queries(const tb_predictor* p, const void* hidden_dev, int32_t n_tokens,
                                         float* scratch_dev, float* q_imp_dev, void* stream);
 
-/* Synchronise `stream`, return the device status word (TB_OK, TB_ERR_TIMEOUT or TB_ERR_BAD_INDEX)
- * in *device_status and clear it. */
+/* Synchronise `stream`, return the device status word (TB_OK, TB_ERR_TIMEOUT or TB_ERR_BAD_INDEX; with device
+ * lengths also TB_ERR_CAPACITY or TB_ERR_UNPROJECTED) in *device_status and clear it. */
 tb_status tb_get_status(tb_ctx* ctx, void* stream, int32_t* device_status);
 
 /* Resident sink and window rows for an offloaded cache (paper Sec. 4.4 "CPU-offloaded KV": the full K/V in

@@ -133,7 +133,7 @@ struct AttnArgs {
 };
 
 constexpr int kStatusCapacity = -3;      // device status: an append in a replayed graph ran past max_seq_len, or a sequence past its launch's room
-constexpr int kStatusUnprojected = -4;   // device status: a replayed selection found candidates that are not projected
+constexpr int kStatusUnprojected = -4;   // device status: a replayed selection found candidates that are not projected, or a compaction kept tokens of which only some are
 
 struct DevState {
     int32_t* len;         // [n_layers * max_batch] device copies of the lengths, advanced by the append kernel

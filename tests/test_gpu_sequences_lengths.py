@@ -1,0 +1,53 @@
+"""Calls on whole sequences whose lengths, or whose lists, only the device knows: replayed appends and forks, and lists that keep nothing."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from test_gpu_fp4 import tb  # noqa: E402,F401
+from test_gpu_sequences import TYPES, grow, lengths, make, raw  # noqa: E402
+
+
+def captured(step):
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    return graph
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("imp,scope", [(32, 0), (16, 2)])
+def test_compaction_does_not_take_replayed_tokens_for_projected_ones(tb, name, imp, scope):
+    """The host believes every token projected, replays have appended some that are not.  Kept among them, the projected length could not say which
+    of the kept tokens are: the sequence is left as it is and reported.  Without kept tokens, or with all of them behind the projected
+    ones, there is nothing to tell apart."""
+    ctx = make(tb, name, hq=8, imp=imp, list_scope=scope)
+    for s in (0, 1, 2):
+        grow(ctx, s, 100)
+    ctx.use_device_lengths(True, growth_reserve=16)
+    k, v = (torch.randn(2, 30, 2, 128, generator=ctx.g, device="cuda").to(ctx.dt) for _ in range(2))
+    graph = captured(lambda: ctx.append_kv(0, 2, [0, 1, 2], [10] * 3, k, v))                # the host counts them, the device has not run it
+    ctx.project_keys(0, 2, [0, 1, 2], None, None, n_seq=3)                # nothing to project yet
+    graph.replay()
+    torch.cuda.synchronize()
+    assert lengths(ctx, 0) == lengths(ctx, 1) == lengths(ctx, 2) == (110, 110)
+    kv, kimp = raw(ctx.kv).clone(), raw(ctx.kimp).clone()
+    idx = torch.tensor([[105, 106, 107, 108, 109]] * 2, dtype=torch.int32, device="cuda")
+    ctx.compact_sequences([0], [90], [5], idx[:1])
+    assert ctx.get_status() == tb.TB_ERR_UNPROJECTED and ctx.get_status() == 0
+    assert torch.equal(raw(ctx.kv), kv) and torch.equal(raw(ctx.kimp), kimp)
+    ctx.compact_sequences([1, 2], [100, 104], [5, 0], idx)
+    assert ctx.get_status() == 0
+    ctx.sync_lengths()
+    assert lengths(ctx, 0) == (110, 100) and lengths(ctx, 1) == (105, 100) and lengths(ctx, 2) == (104, 100)
+    # what is projected now is what a sequence of those tokens projects to
+    ctx.project_keys(0, 2, [0, 1, 2], None, None, n_seq=3)
+    ctx.sync_lengths()
+    for s, m in ((0, 110), (1, 105), (2, 104)):
+        assert lengths(ctx, s) == (m, m)
+        kimp = ctx.kimp[:, s, :, :m].clone()
+        ctx.kimp[:, s] = 0
+        ctx.project_keys(0, 2, [s], [0], [m])
+        assert torch.equal(ctx.kimp[:, s, :, :m], kimp)
+    assert ctx.get_status() == 0
