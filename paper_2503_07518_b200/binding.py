@@ -248,7 +248,8 @@ class Context:
             raise TBError(st, "tb_append_kv")
 
     def read_kv(self, layer_begin, layer_count, seq_ids, pos_begin, pos_end, k_out, v_out, stream=None):
-        """K and V rows of positions [pos_begin[i], pos_end[i]) into k_out, v_out [layer_count, sum of them, kv heads, head dim]."""
+        """K and V rows of positions [pos_begin[i], pos_end[i]) into k_out, v_out [layer_count, sum of them, kv heads, head dim]
+        of the type that append_kv takes (a tensor with less room is refused)."""
         st = _calls.read_kv(self._address, layer_begin, layer_count, seq_ids, pos_begin, pos_end, k_out, v_out, stream)
         if st:
             raise TBError(st, "tb_read_kv")

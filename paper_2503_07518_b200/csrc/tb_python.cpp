@@ -19,7 +19,7 @@
 #include <cstdint>
 #include <vector>
 
-#include "../../include/tokenbutler.h"
+#include "tb_internal.h"      // (a context's configuration)
 
 // Read from the file by build.py and binding.py: another torch or Python needs another build.
 extern "C" __attribute__((used, visibility("default"))) const char tb_calls_abi[] = TB_CALLS_ABI;
@@ -171,14 +171,18 @@ PyObject* append_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return call([&] { return tb_append_kv((tb_ctx*)ctx, lb, lc, ids.data, n_new.data, (int32_t)n_new.n, k, v, stream); });
 }
 
-// What a kernel reads or writes as one run of bytes: a torch tensor has to be one, on a device, and of the type that is asked for.
-bool is_dense(PyObject* o, bool ints, const char* what) {
+// What a kernel reads or writes as one run of bytes: a torch tensor has to be one, of the type that is asked for, on the context's device (on
+// any device where there is no context to ask).
+bool is_dense(PyObject* o, const void* ctx, at::ScalarType type, const char* what) {
     if (!THPVariable_Check(o)) return true;
     const at::Tensor& t = THPVariable_Unpack(o);
-    if (t.is_cuda() && t.is_contiguous() && (!ints || t.scalar_type() == at::kInt)) return true;
-    PyErr_Format(PyExc_ValueError, "%s: a contiguous %sCUDA tensor is expected", what, ints ? "int32 " : "");
+    if (t.is_cuda() && t.is_contiguous() && t.scalar_type() == type && (!ctx || t.get_device() == ((const tb_ctx*)ctx)->cfg.device)) return true;
+    PyErr_Format(PyExc_ValueError, "%s: a contiguous %s tensor on the context's device is expected", what, at::toString(type));
     return false;
 }
+
+// Whether a tensor that a kernel fills has room (anything that is no torch tensor is taken at its word).
+bool has_room(PyObject* o, int64_t elements) { return !THPVariable_Check(o) || THPVariable_Unpack(o).numel() >= elements; }
 
 // (ctx, layer_begin, layer_count, seq_ids, pos_begin, pos_end, k_out, v_out, stream)
 PyObject* read_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -188,7 +192,13 @@ PyObject* read_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!want(n, 9) || !read_address(a[0], &ctx) || !read_int(a[1], &lb) || !read_int(a[2], &lc) || !ids.read(a[3]) || !pb.read(a[4]) ||
         !pe.read(a[5]) || !read_pointer(a[6], &k) || !read_pointer(a[7], &v) || !read_stream(a[8], &stream))
         return nullptr;
-    if (!same_length(ids, pb) || !same_length(pe, pb) || !is_dense(a[6], false, "k_out") || !is_dense(a[7], false, "v_out")) return nullptr;
+    const tb_config* cfg = ctx ? &((const tb_ctx*)ctx)->cfg : nullptr;
+    const at::ScalarType type = cfg && cfg->kv_dtype == TB_F32 ? at::kFloat : at::kBFloat16;
+    if (!same_length(ids, pb) || !same_length(pe, pb) || !is_dense(a[6], ctx, type, "k_out") || !is_dense(a[7], ctx, type, "v_out")) return nullptr;
+    int64_t tokens = 0;
+    for (Py_ssize_t i = 0; pe.data && i < pb.n; ++i) tokens += pe.data[i] > pb.data[i] ? (int64_t)pe.data[i] - pb.data[i] : 0;
+    const int64_t elements = cfg && lc > 0 ? tokens * lc * cfg->n_kv_heads * cfg->head_dim : 0;
+    if (!has_room(a[6], elements) || !has_room(a[7], elements)) return PyLong_FromLong(TB_ERR_INVALID_ARG);
     return call([&] { return tb_read_kv((tb_ctx*)ctx, lb, lc, ids.data, pb.data, pe.data, (int32_t)pb.n, k, v, stream); });
 }
 
@@ -211,7 +221,7 @@ PyObject* compact_sequences(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (!want(n, 6) || !read_address(a[0], &ctx) || !ids.read(a[1]) || !begin.read(a[2]) || !keep.read(a[3]) ||
         (a[4] != Py_None && !read_matrix(a[4], &idx, &rows, &stride)) || !read_stream(a[5], &stream))
         return nullptr;
-    if (!same_length(ids, begin) || !same_length(keep, begin) || !is_dense(a[4], true, "keep_idx")) return nullptr;
+    if (!same_length(ids, begin) || !same_length(keep, begin) || !is_dense(a[4], ctx, at::kInt, "keep_idx")) return nullptr;
     if (idx && rows < (int32_t)begin.n) {
         PyErr_SetString(PyExc_ValueError, "a row of positions per sequence is expected");
         return nullptr;
