@@ -161,7 +161,7 @@ tb_status tb_append_kv(tb_ctx* ctx, int32_t layer_begin, int32_t layer_count, co
 /* Rows out of the cache as values, the inverse of tb_append_kv: positions [pos_begin[i], pos_end[i]) of each listed sequence for layers
  * [layer_begin, layer_begin+layer_count) go to k_out, v_out [layer_count][sum(pos_end - pos_begin)][Hkv][D] in the type that tb_append_kv takes
  * (TB_FP4: bf16, exact).  What attention among the tokens of a prompt has to use when the cache does not hold them as they came.
- * Positions must be cached (TB_ERR_INVALID_ARG); k_out, v_out 16-byte aligned device memory, not inside the cache. */
+ * Positions must be cached (TB_ERR_INVALID_ARG); k_out, v_out 16-byte aligned device memory, not inside the cache (NULL only where no token is read). */
 tb_status tb_read_kv(tb_ctx* ctx, int32_t layer_begin, int32_t layer_count, const int32_t* seq_ids, const int32_t* pos_begin,
                      const int32_t* pos_end, int32_t n_seq, void* k_out_dev, void* v_out_dev, void* stream);
 
@@ -177,8 +177,8 @@ tb_status tb_fork_sequence(tb_ctx* ctx, int32_t src_seq, const int32_t* dst_seqs
 /* Drops tokens of the listed sequences in place, in every layer (rejected drafts, rollback, a branch that keeps part of its context):
  * tokens before keep_begin[i] stay, then come the n_keep[i] tokens at positions keep_idx_dev[i][0..n_keep[i]), which ascend strictly and lie in
  * [keep_begin[i], length); the rest is gone and the length is keep_begin[i] + n_keep[i].  keep_idx_dev [n_seq][keep_stride] int32, device
- * memory; n_keep == keep_idx_dev == NULL keeps nothing behind keep_begin (truncation: without device lengths or resident rows no kernel
- * runs).  Rows and projected keys move, bit for bit; rows behind the new length are left as they are.  A layer's stored
+ * memory, which may be NULL where every n_keep is 0.  n_keep all 0, or n_keep == keep_idx_dev == NULL, keeps nothing behind keep_begin (truncation:
+ * without device lengths or resident rows no kernel runs).  Rows and projected keys move, bit for bit; rows behind the new length are left as they are.  A layer's stored
  * selection stays if it was made while the layer held at most keep_begin[i] tokens (without device lengths), else it is dropped.  Bound resident rows are brought up to date.
  * An entry that does not ascend or lies outside the range sets TB_ERR_BAD_INDEX in the status word; its row holds what it held before.
  * With device lengths the counts are still those given here.  A layer of a sequence that is shorter than they say keeps its rows and length, and is reported as

@@ -571,7 +571,7 @@ tb_status tb_sparse_decode_attention(tb_ctx* c, int32_t lb, int32_t lc, const in
 
 tb_status tb_read_kv(tb_ctx* c, int32_t lb, int32_t lc, const int32_t* seq_ids, const int32_t* pos_begin, const int32_t* pos_end,
                      int32_t n_seq, void* k_out, void* v_out, void* stream) {
-    if (!c || !pos_begin || !pos_end || !k_out || !v_out || bad_layers(c, lb, lc)) return TB_ERR_INVALID_ARG;
+    if (!c || !pos_begin || !pos_end || bad_layers(c, lb, lc)) return TB_ERR_INVALID_ARG;
     if (((uintptr_t)k_out | (uintptr_t)v_out) & 15) return TB_ERR_INVALID_ARG;
     int seqs[kMaxLaunchSeq];
     const tb_status st = resolve_seqs(c, seq_ids, n_seq, seqs);
@@ -589,7 +589,8 @@ tb_status tb_read_kv(tb_ctx* c, int32_t lb, int32_t lc, const int32_t* seq_ids, 
         if ((total += n) > 2147483647LL) return TB_ERR_CAPACITY;
         rt.pos_begin[i] = pos_begin[i], rt.tok_off[i + 1] = (int)total;
     }
-    if (longest == 0) return TB_OK;
+    if (longest == 0) return TB_OK;                    // (an empty tensor has no address)
+    if (!k_out || !v_out) return TB_ERR_INVALID_ARG;
     const size_t layer_stride = (size_t)total * c->cfg.n_kv_heads * c->cfg.head_dim * elem_size(c->cfg.kv_dtype);
     const int step = layers_per_launch(n_seq);
     for (int l0 = lb; l0 < lb + lc; l0 += step) {
@@ -665,7 +666,7 @@ tb_status tb_fork_sequence(tb_ctx* c, int32_t src, const int32_t* dst, int32_t n
 
 tb_status tb_compact_sequences(tb_ctx* c, const int32_t* seq_ids, int32_t n_seq, const int32_t* keep_begin, const int32_t* n_keep,
                                const int32_t* keep_idx, int32_t keep_stride, void* stream) {
-    if (!c || !keep_begin || (n_keep == nullptr) != (keep_idx == nullptr)) return TB_ERR_INVALID_ARG;
+    if (!c || !keep_begin || (keep_idx && !n_keep)) return TB_ERR_INVALID_ARG;
     int seqs[kMaxLaunchSeq];
     const tb_status st = resolve_seqs(c, seq_ids, n_seq, seqs);
     if (st != TB_OK) return st;
@@ -674,7 +675,7 @@ tb_status tb_compact_sequences(tb_ctx* c, const int32_t* seq_ids, int32_t n_seq,
     a.keep = keep_idx, a.stride = keep_stride, a.max_keep = 0;
     for (int i = 0; i < n_seq; ++i) {
         const int n = n_keep ? n_keep[i] : 0;
-        if (keep_begin[i] < 0 || n < 0 || (n > 0 && n > keep_stride)) return TB_ERR_INVALID_ARG;
+        if (keep_begin[i] < 0 || n < 0 || (n > 0 && (!keep_idx || n > keep_stride))) return TB_ERR_INVALID_ARG;
         a.begin[i] = keep_begin[i], a.n_keep[i] = n;
         if (n > a.max_keep) a.max_keep = n;
         for (int l = 0; l < layers; ++l) {

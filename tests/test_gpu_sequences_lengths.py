@@ -51,3 +51,27 @@ def test_compaction_does_not_take_replayed_tokens_for_projected_ones(tb, name, i
         ctx.project_keys(0, 2, [s], [0], [m])
         assert torch.equal(ctx.kimp[:, s, :, :m], kimp)
     assert ctx.get_status() == 0
+
+
+@pytest.mark.parametrize("name", TYPES)
+def test_lists_and_ranges_with_nothing_in_them(tb, name):
+    """A round that keeps no draft, and a read of no tokens, as a program that sizes its tensors by their counts calls them."""
+    ctx = make(tb, name, batch=3)
+    grow(ctx, 0, 40)
+    grow(ctx, 2, 30)
+    kv, n0 = raw(ctx.kv).clone(), ctx.launch_count()
+    none = torch.empty(2, 0, dtype=torch.int32, device="cuda")
+    ctx.compact_sequences([2, 0], [25, 40], [0, 0], none)
+    assert lengths(ctx, 2) == (25, 25) and lengths(ctx, 0) == (40, 40)
+    out = torch.empty(2, 0, 2, 128, dtype=ctx.dt, device="cuda")
+    ctx.read_kv(0, 2, [0, 2], [7, 25], [7, 25], out, out)
+    assert ctx.launch_count() == n0 and torch.equal(raw(ctx.kv), kv) and ctx.get_status() == 0
+    for call, a in ((ctx.compact_sequences, ([0], [10], [1], none)), (ctx.compact_sequences, ([2, 0], [0, 0], [0, 1], none)),
+                    (ctx.read_kv, (0, 2, [0], [7], [8], out, out)), (ctx.read_kv, (0, 2, [0], [41], [41], out, out)), (ctx.read_kv, (0, 2, [0], [8], [7], out, out))):
+        with pytest.raises(tb.TBError) as e:
+            call(*a)
+        assert e.value.status == tb.TB_ERR_INVALID_ARG and ctx.launch_count() == n0
+    ctx.use_device_lengths(True, 0)
+    ctx.compact_sequences([0], [33], [0], none[:1])
+    ctx.sync_lengths()
+    assert lengths(ctx, 0) == (33, 33) and ctx.get_status() == 0
