@@ -170,7 +170,8 @@ tb_status tb_read_kv(tb_ctx* ctx, int32_t layer_begin, int32_t layer_count, cons
  * n_tokens < 0 copies all tokens and the stored selections too (a sample can go on in the middle of an interval); otherwise the copies have
  * no selection yet.  What the slots held is gone; the source is unchanged.  The bound resident rows and the Important buffer of the copies are
  * brought up to date.  With device lengths the source's counters are read, and the copies' written, on the device: n_tokens < 0 can be
- * captured and replayed while the source grows.
+ * captured and replayed while the source grows, and brings the lists that the source then has.  (Whether a slot has a selection to reuse is what the
+ * host's own calls say, here as for tb_compact_sequences: replays do not change it.  Select again where a replay has moved or replaced what a list names.)
  * TB_ERR_INVALID_ARG: a slot out of range, twice in dst_seqs or equal to the source, more tokens than a layer holds; TB_ERR_UNSUPPORTED: over 64 slots. */
 tb_status tb_fork_sequence(tb_ctx* ctx, int32_t src_seq, const int32_t* dst_seqs, int32_t n_dst, int32_t n_tokens, void* stream);
 

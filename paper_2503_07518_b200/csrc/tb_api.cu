@@ -633,11 +633,11 @@ tb_status tb_fork_sequence(tb_ctx* c, int32_t src, const int32_t* dst, int32_t n
     for (int i = 0; i < n_dst; ++i)
         if (a.dst[i] == src) return TB_ERR_INVALID_ARG;
     const int mb = c->cfg.max_batch, layers = c->cfg.n_layers;
-    bool selected = false, cached = c->dev_lengths != 0;
+    bool cached = c->dev_lengths != 0;
     for (int l = 0; l < layers; ++l) {
         const size_t u = (size_t)l * mb + src;
         if (n_tokens > c->len[u]) return TB_ERR_INVALID_ARG;
-        selected |= n_tokens < 0 && c->has_sel[u], cached |= c->len[u] > 0 && n_tokens != 0;
+        cached |= c->len[u] > 0 && n_tokens != 0;
     }
     a.src = src, a.n_dst = n_dst, a.n_tokens = n_tokens < 0 ? -1 : n_tokens;
     const int step = layers_per_launch(1);
@@ -661,7 +661,8 @@ tb_status tb_fork_sequence(tb_ctx* c, int32_t src, const int32_t* dst, int32_t n
             c->has_sel[d] = n_tokens < 0 ? c->has_sel[u] : 0;
             c->sel_cnt[d] = n_tokens < 0 ? c->sel_cnt[u] : -1, c->sel_len[d] = c->sel_len[u];
         }
-    return cached ? refresh_copies(c, a.dst, n_dst, selected, (cudaStream_t)stream) : TB_OK;
+    // (where lists are copied so are their rows, whether or not there is a selection now: a replay copies the lists of its time)
+    return cached ? refresh_copies(c, a.dst, n_dst, n_tokens < 0, (cudaStream_t)stream) : TB_OK;
 }
 
 tb_status tb_compact_sequences(tb_ctx* c, const int32_t* seq_ids, int32_t n_seq, const int32_t* keep_begin, const int32_t* n_keep,

@@ -1,4 +1,6 @@
 """Calls on whole sequences whose lengths, or whose lists, only the device knows: replayed appends and forks, and lists that keep nothing."""
+import math
+
 import pytest
 import torch
 
@@ -75,3 +77,26 @@ def test_lists_and_ranges_with_nothing_in_them(tb, name):
     ctx.compact_sequences([0], [33], [0], none[:1])
     ctx.sync_lengths()
     assert lengths(ctx, 0) == (33, 33) and ctx.get_status() == 0
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("devlen", [False, True])
+def test_a_fork_captured_before_the_first_selection_brings_the_rows_of_later_ones(tb, name, devlen):
+    """Beams: the copy is captured once, then source and copy are selected, and the copy replaced by the source's state.  With an Important
+    buffer its rows are those of the lists that came with it."""
+    ctx = make(tb, name, hq=8, batch=2, room=300, budget=24)
+    ctx.bind_important_buffer()
+    grow(ctx, 0, 200)
+    grow(ctx, 1, 200)
+    if devlen:
+        ctx.use_device_lengths(True, growth_reserve=0)
+    graph = captured(lambda: ctx.fork_sequence(0, [1]))
+    qi = torch.randn(2, 2, 8, 32, generator=ctx.g, device="cuda")
+    q = torch.randn(2, 1, 8, 128, generator=ctx.g, device="cuda").to(ctx.dt).expand(-1, 2, -1, -1).contiguous()
+    p = tb.select_params(24, 4, 16)
+    ctx.select_topk(0, 2, None, 2, qi, p)
+    graph.replay()
+    out = torch.full((2, 2, 8, 128), math.nan, device="cuda")
+    ctx.sparse_decode_attention(0, 2, None, 2, q, p, out)
+    assert torch.isfinite(out).all() and torch.equal(out[:, 0], out[:, 1])
+    assert ctx.get_status() == 0
