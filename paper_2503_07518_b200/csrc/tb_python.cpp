@@ -222,6 +222,10 @@ PyObject* compact_sequences(PyObject*, PyObject* const* a, Py_ssize_t n) {
         (a[4] != Py_None && !read_matrix(a[4], &idx, &rows, &stride)) || !read_stream(a[5], &stream))
         return nullptr;
     if (!same_length(ids, begin) || !same_length(keep, begin) || !is_dense(a[4], ctx, at::kInt, "keep_idx")) return nullptr;
+    if (THPVariable_Check(a[4]) && THPVariable_Unpack(a[4]).dim() != 2) {      // (a stride is one size: the rows of any other shape would be read elsewhere)
+        PyErr_SetString(PyExc_ValueError, "keep_idx: a matrix is expected");
+        return nullptr;
+    }
     if (idx && rows < (int32_t)begin.n) {
         PyErr_SetString(PyExc_ValueError, "a row of positions per sequence is expected");
         return nullptr;

@@ -100,3 +100,19 @@ def test_a_fork_captured_before_the_first_selection_brings_the_rows_of_later_one
     ctx.sparse_decode_attention(0, 2, None, 2, q, p, out)
     assert torch.isfinite(out).all() and torch.equal(out[:, 0], out[:, 1])
     assert ctx.get_status() == 0
+
+
+def test_positions_come_as_a_matrix(tb):
+    """Two sequences' lists in any other shape: refused, not read from the wrong places."""
+    ctx = make(tb, "fp4", batch=2)
+    grow(ctx, 0, 40)
+    grow(ctx, 1, 40)
+    idx, n0 = torch.arange(32, dtype=torch.int32, device="cuda").view(2, 16), ctx.launch_count()
+    for bad in (idx.view(2, 4, 4), idx.view(2, 16, 1), idx.view(1, 2, 16)):
+        with pytest.raises(ValueError, match="keep_idx"):
+            ctx.compact_sequences([0, 1], [0, 0], [3, 3], bad)
+    with pytest.raises((ValueError, IndexError)):
+        ctx.compact_sequences([0], [0], [3], idx.view(-1))
+    assert ctx.launch_count() == n0 and lengths(ctx, 0) == lengths(ctx, 1) == (40, 40)
+    ctx.compact_sequences([0, 1], [0, 0], [3, 3], idx)
+    assert lengths(ctx, 1) == (3, 3) and ctx.get_status() == 0
