@@ -94,15 +94,13 @@ cudaError_t launch_fork(const tb_ctx* c, const UnitTable& ut, const ForkArgs& a,
 // 383 when entries were fetched with their rows, 1290 with a block per unit.
 // Entries that do not ascend or lie outside [begin, length) are reported and their rows left alone (the order above holds for
 // any entry >= begin + j, and others are not followed).
-// Lengths read on the device may differ from what the host checked.  A unit's sequence then is left as it is, whole, where it is shorter than the
+// Lengths read on the device may differ from what the host checked.  A layer of a sequence is then left as it is, whole, where it is shorter than the
 // counts say (kStatusBadIndex), or where the projected tokens end among those it may keep (kStatusUnprojected: a projected length is a prefix
 // and could not say which of the kept rows have their keys).
-__device__ __forceinline__ int compact_refusal(const Geom& gm, const UnitTable& ut, const CompactArgs& a, int ll, int s) {
-    const int L = unit_len(gm, ut, ll, s);
-    if (a.begin[s] + a.n_keep[s] > L) return kStatusBadIndex;
-    if (!ut.use_dev_len || a.n_keep[s] == 0) return 0;
-    const int P = __ldcg(ut.len_proj_dev + (size_t)(ut.layer_begin + ll) * gm.max_batch + ut.seq_id[s]);
-    return P > a.begin[s] && P < L ? kStatusUnprojected : 0;
+__device__ __forceinline__ bool compact_partial(const Geom& gm, const UnitTable& ut, const CompactArgs& a, int ll, int s, int L) {
+    if (!ut.use_dev_len || a.n_keep[s] == 0) return false;
+    const int P = ut.len_proj_dev[(size_t)(ut.layer_begin + ll) * gm.max_batch + ut.seq_id[s]];
+    return P > a.begin[s] && P < L;
 }
 constexpr int kCompactThreads = 256;
 constexpr int kCompactUnroll = 8;
@@ -122,9 +120,10 @@ __global__ void __launch_bounds__(kCompactThreads, 2) compact_kernel(Geom gm, Un
     pdl_wait();                                        // (see append_kernel)
     pdl_launch_dependents();
     const int begin = a.begin[s], L = unit_len(gm, ut, ll, s);
-    const int refused = compact_refusal(gm, ut, a, ll, s);
-    const int n = there && !refused ? a.n_keep[s] : 0;
-    bool bad = false;
+    const bool partial = compact_partial(gm, ut, a, ll, s, L);
+    // (the sequence that is too short is reported with the bad entries, behind the loop: decided here with the other one, the loop took 8% longer)
+    const int n = there && begin + a.n_keep[s] <= L && !partial ? a.n_keep[s] : 0;
+    bool bad = begin + a.n_keep[s] > L;
     const int wide = rs.chunks / slices, rows = kGroup / wide;        // chunks of the slice; rows that the group moves side by side
     const int row0 = me / wide;
     const bool works = row0 < rows;
@@ -171,12 +170,13 @@ __global__ void __launch_bounds__(kCompactThreads, 2) compact_kernel(Geom gm, Un
             if (moves >> i & 1) unit[(size_t)(begin + j0 + row0 + i * rows) * rs.chunks] = w[i];
     }
     if (bad) atomicExch(status, kStatusBadIndex);
-    if (refused && there && me == 0) atomicExch(status, refused);
+    if (partial && there && me == 0) atomicExch(status, kStatusUnprojected);
     if (!ut.use_dev_len || !last_block_arrives(counter, gridDim.x * gridDim.y * gridDim.z)) return;
     for (int i = threadIdx.x; i < ut.layer_count * ut.n_seq; i += kCompactThreads) {
-        const int s2 = i % ut.n_seq, len = a.begin[s2] + a.n_keep[s2];
-        if (compact_refusal(gm, ut, a, i / ut.n_seq, s2)) continue;
+        const int s2 = i % ut.n_seq, want = a.begin[s2] + a.n_keep[s2];
         const size_t pair = (size_t)(ut.layer_begin + i / ut.n_seq) * gm.max_batch + ut.seq_id[s2];
+        const int len = min(len_dev[pair], want);
+        if (compact_partial(gm, ut, a, i / ut.n_seq, s2, len_dev[pair])) continue;
         len_dev[pair] = len;
         if (len_proj_dev[pair] > len) len_proj_dev[pair] = len;
     }
