@@ -378,10 +378,11 @@ __device__ __forceinline__ void f32_rows(const float* __restrict__ qbase, int g,
 //   Row r of a tile is token r for even r < 8, 8 + (r + 3) % 8 for odd r < 8, one more than row r - 8's for the others: 144-byte rows,
 //   unpadded, then hit distinct banks in both reads.
 // Queries are bf16: scaled by a power of two per head that brings the largest channel to [2^13, 2^14), every channel down to 2^-28 of
-// it is exact in f16 and the rest is off by less than 2^-39 of it.
+// it is exact in f16 and the rest is off by at most 2^-38 of it (half a subnormal step, 2^-25, beside at least 2^13).
 // Weights are 2^(x - ref): ref is the running maximum less 13 and follows only once a score is more than 15.9 above it, so that most tiles
-// need no reduction over the lanes and no rescaling.  They are split into an f16 high and low part: 22 bits for all but those below 2^-27 of
-// the largest, which are off by less than 2^-38 of it.  With up to four heads (kNarrow) columns 4..7 repeat heads 0..3 in S and take the low parts in O:
+// need no reduction over the lanes and no rescaling.  They are split into an f16 high and low part.  The largest is at least 2^13 and the low
+// part's steps end at 2^-24: 22 bits down to 2^-16 of the largest weight, below that a weight is off by at most 2^-25, that is 2^-38 of the
+// largest (20 bits at 2^-18 of it, 11 at 2^-27).  With up to four heads (kNarrow) columns 4..7 repeat heads 0..3 in S and take the low parts in O:
 // one mma where five to eight heads need two.
 // The tensor core truncates as it accumulates, about 2e-8 of the sum per mma, which adds up over the tiles of a long sequence (3.8e-6 of the
 // result at 120,000 tokens).  So O moves into fp32 sums in shared memory every kFp4Flush tiles; adding every pair of tiles in registers took
@@ -389,7 +390,8 @@ __device__ __forceinline__ void f32_rows(const float* __restrict__ qbase, int g,
 // What bounds it: the conversions, their scaling (64 lanes per clock each) and the mma together take 4.3 clocks of an SM per row, the rest two more,
 // and a row's 144 bytes six at the copy bandwidth: 16 problems of 110,000 rows 59.5 us, 65% of it; the bf16 rows of the same tokens 131.
 // Gathered rows cost 192 bytes of DRAM each (three accesses of 64), and a launch of them a chain of lists, rows, two or three tiles per warp
-// and a merge.
+// and a merge.  For one sequence that chain is what counts and bf16 rows have the shorter one (8 problems of 3276 listed rows out of DRAM: 7.2 us, bf16
+// 5.3); from about four sequences the bytes do (32 problems: 11.4 and 12.3; 256 of 3276: 42 and 71).
 // Leaves accumulators and statistics parked as the bf16 warp does, but for the channels: float4 number mt * 32 + lane holds
 // channels 16 gid + 2 mt and + 1 (kNarrow: of heads 2 tig and + 1 in lanes tig < 2, their low parts in lanes tig + 2).
 constexpr int kFp4Tile = 32;                          // rows of a stage
@@ -1532,7 +1534,9 @@ extern "C" tb_status tb_sparse_decode_attention_static(const void* kv_dev, int32
     for (int i = 0; i < n_seq; ++i) a.known_cnt[i] = -1;
     a.sm_scale = sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)head_dim);
     {   // about four 4-warp blocks per SM, at least 64 rows per split; no clusters here: the splits
-        // always merge through the scratch array (last block to arrive, fixed order)
+        // always merge through the scratch array (last block to arrive, fixed order).  4-bit rows take the same
+        // splits although a warp's tile has 32 of them (1 sequence, 8 KV heads, 3276 listed rows: 14.7 us, bf16 13.3;
+        // 2 of 819: 12.5 and 12.6; every row of 2 x 32768: 31 and 64)
         int units = n_seq * n_kv_heads, target = 4 * sm_count;
         int n = (target + units - 1) / units, by_rows = max_rows / 64;
         if (n > by_rows) n = by_rows;

@@ -139,12 +139,13 @@ cudaError_t launch_read_fp4(const tb_ctx* c, const UnitTable& ut, const ReadTabl
 // takes its channels 32 tig + 4 ks + (0, 1 | 2, 3).  The rows of W_K are fetched in the same order, its columns placed so that a lane ends with
 // consecutive outputs of its two tokens.
 // Codes become f16 pairs and are scaled there, exactly.  W_K is bf16; a warp that walks brings its matrix to f16 too, by a power of two that puts
-// the largest element in [2^13, 2^14): exact for elements down to 2^-31 of it.  Where one is smaller, and for few tokens, the keys are turned
+// the largest element in [2^13, 2^14): exact for elements down to 2^-30 of it.  Where one is smaller, and for few tokens, the keys are turned
 // into bf16 instead, also exactly, which costs three instructions per pair (1M rows x d' 32: 53 us like that, 43 on f16).  The products and the
 // order of their sums are the same, and so are the results; one rounding, at the end.
 // kWalk: a block keeps the matrix in registers and walks over the tokens, each warp a tile of 16 at a time with the next kProjAhead on their
 // way.  Otherwise (few tokens per unit, or one key stream per layer, which sums the heads' projections) it is read from shared memory,
-// two tiles at a time, and twice as many blocks are resident.
+// two tiles at a time, and twice as many blocks are resident.  One key stream per layer brings a head's matrix into shared memory for every 128
+// tokens, behind two barriers, which bounds it: 4 layers of 32768 tokens of 8 heads, d' 32, 72 us (bf16 rows 51; a stream per head 39).
 // Bound by DRAM: of a row's 144 bytes 96 are asked for (three sectors), but memory is read 64 bytes at a time and that is all of it, so 144 in and
 // 2 d' out: 1M rows, d' 32, 218 MB in 41 us (5.3 TB/s); rows prefetched into registers 46, 64 tokens and a matrix per block 99.
 constexpr int kProjFp4Threads = 128;
