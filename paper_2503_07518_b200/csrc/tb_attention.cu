@@ -1535,8 +1535,8 @@ extern "C" tb_status tb_sparse_decode_attention_static(const void* kv_dev, int32
     a.sm_scale = sm_scale > 0.f ? sm_scale : 1.0f / sqrtf((float)head_dim);
     {   // about four 4-warp blocks per SM, at least 64 rows per split; no clusters here: the splits
         // always merge through the scratch array (last block to arrive, fixed order).  4-bit rows take the same
-        // splits although a warp's tile has 32 of them (1 sequence, 8 KV heads, 3276 listed rows: 14.7 us, bf16 13.3;
-        // 2 of 819: 12.5 and 12.6; every row of 2 x 32768: 31 and 64)
+        // splits although a warp's tile has 32 of them (1 sequence, 8 KV heads, 3276 listed rows, in L2: 14.7
+        // us, bf16 13.3; 2 of 819: 12.5 and 12.6; every row of 2 x 32768: 31 and 64)
         int units = n_seq * n_kv_heads, target = 4 * sm_count;
         int n = (target + units - 1) / units, by_rows = max_rows / 64;
         if (n > by_rows) n = by_rows;
