@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kCompactThreads, 2) compact_kernel(Geom gm, Un
     pdl_launch_dependents();
     const int begin = a.begin[s], L = unit_len(gm, ut, ll, s);
     const bool partial = compact_partial(gm, ut, a, ll, s, L);
-    // (the sequence that is too short is reported with the bad entries, behind the loop: decided here with the other one, the loop took 8% longer)
+    // (the sequence that is too short is reported with the bad entries, behind the loop: decided here with the other one, the loop took 9% longer)
     const int n = there && begin + a.n_keep[s] <= L && !partial ? a.n_keep[s] : 0;
     bool bad = begin + a.n_keep[s] > L;
     const int wide = rs.chunks / slices, rows = kGroup / wide;        // chunks of the slice; rows that the group moves side by side
